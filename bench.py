@@ -33,7 +33,7 @@ HBM_PEAK_GBS = 8000.0
 # with.  The same counters read 303,884 (FETCH_SIZE) and 607,744 (WRITE_SIZE) for a device-to-device copy of 607,744 KiB,
 # hence the scale factors to KiB.  The summaries under profiles/ hold the commands and the full tables.
 PMC = {
-    "sources_sha256": "0b6ab2dce900fa4a48f3ecb531ed80aceade5e926bdd75eaeed1adee0352575e",
+    "sources_sha256": "8d799024e988177a288f57bd3880dbb663c907b5f9680bde172253c616f84f94",
     "fetch_scale": 2.00, "write_scale": 1.00,
     "k_build": (11022.0, 4800.5),
     "k_fill": (3409.4, 19287.3),

@@ -12,6 +12,9 @@
  *                                                       Generation Algorithm" (runtime combination)
  *   apply_token_bitmask(logits[B, V], bitmask)          section 2.1 (invalid tokens get -infinity)
  *
+ * and, for a search that keeps several continuations of a sequence at a time, the operators that choose from the masked
+ * logits and let matchers, caches and outputs follow the choice (xg2_beam_*, xg2_batch_reorder).
+ *
  * Conventions
  *   - Every call returns an int32 status: XG2_OK or a negative XG2_E* code; the text of the last
  *     error of the calling thread is returned by xg2_last_error().
@@ -302,6 +305,62 @@ int32_t xg2_batch_row_info(xg2_batch*, int32_t row, int32_t* info_host);
 #define XG2_BF16 1
 int32_t xg2_apply_token_bitmask(void* logits_dev, int32_t dtype, int32_t B, int32_t V, int64_t row_stride_elems,
                                 const int32_t* bitmask_dev, int64_t bm_row_stride_words, void* hip_stream);
+
+/* ---- beam search under a grammar -----------------------------------------------------------------
+ * G groups (requests) of K beams each; row g * K + k of every array is beam k of group g.  One step of a search whose
+ * matchers live on the device:
+ *     xg2_batch_fill_next_token_bitmask -> xg2_beam_select -> xg2_batch_reorder, xg2_beam_reorder_rows -> xg2_batch_accept_tokens
+ * with n_out = K, the chosen parents handed to both reorderings and the chosen tokens to accept (-1 there means none, as it
+ * does for a beam that has ended).  All calls only enqueue kernels, allocate nothing and may be captured into a graph; what
+ * they work with belongs to the caller, so calls on different buffers may overlap.  K is between 1 and 64, G * K at most 2^20.
+ *
+ * The best n_out candidates of every group.  A candidate is an allowed token of a row whose beam goes on; its score is
+ *     scores[row] + logits[row, token] - log(sum over the tokens that count of exp(logits[row, .])),
+ * over = XG2_OVER_ALLOWED: the allowed tokens of the row count (probabilities given that the grammar is kept to);
+ * XG2_OVER_ALL: all V tokens count (the model's own probabilities).  A beam that has ended (finished[row] != 0; finished_dev
+ * may be NULL) is one candidate: its score as it is, with token -1.  Chosen are the largest scores, among equal ones the lowest
+ * row, in it the lowest token.  Scores are compared as sums in 64 bits give them.
+ *   logits_dev: G * K rows of row_stride_elems elements (XG2_F32 or XG2_BF16), at a multiple of the element's size; not written.
+ *   bitmask_dev: rows of bm_row_stride_words words as xg2_batch_fill_next_token_bitmask writes them, or NULL: all are allowed.
+ *   scores_dev: float32 per row; -infinity (also +infinity and NaN): no beam, the row is not read.
+ * A row that allows nothing has no candidates.  A logit of NaN or -infinity is no candidate and does not count; where
+ * +infinity counts, the tokens that have it share the probability evenly and the others have none.
+ * Out, [G, n_out] each, best first: scores, parents (rows), tokens, and (may be NULL) whether the continuation has ended:
+ * 1 if its parent had or its token is eos_id.  Where a group has fewer candidates the rest is -infinity, -1, -1, 1.
+ * n_out is between 1 and 128, V at most 2^30.  No output may overlap an input.  workspace_dev: device, 16-byte aligned, at
+ * least as many bytes as xg2_beam_select_workspace says, which later calls may use again in stream order.                  */
+#define XG2_OVER_ALLOWED 0
+#define XG2_OVER_ALL     1
+int32_t xg2_beam_select_workspace(int32_t dtype, int32_t groups, int32_t beams, int32_t V, int32_t n_out, size_t* bytes);
+int32_t xg2_beam_select(const void* logits_dev, int32_t dtype, int32_t groups, int32_t beams, int32_t V, int64_t row_stride_elems,
+                        const int32_t* bitmask_dev, int64_t bm_row_stride_words, int32_t over, const float* scores_dev,
+                        const int32_t* finished_dev, int32_t eos_id, int32_t n_out, float* out_scores_dev, int32_t* out_parents_dev,
+                        int32_t* out_tokens_dev, int32_t* out_finished_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* Every slot b of the batch takes over the state that slot parents_dev[b] had before the call (its parser, its cache, whether
+ * it has terminated, a sticky error): several slots may name the same parent, -1 keeps the slot's state.  The batch is divided
+ * into groups of `beams` slots (its number of slots is a multiple), and a parent lies in its slot's own group.
+ * parents_dev: device, B int32.  status_dev (device, B int32, may be NULL): XG2_OK, or XG2_EINVAL for a parent outside the
+ * group, whose slot keeps its state.                                                                                       */
+int32_t xg2_batch_reorder(xg2_batch*, int32_t beams, const int32_t* parents_dev, int32_t* status_dev, void* hip_stream);
+
+/* In place: the beams' rows of a buffer (attention cache, token history) take over what their parents' rows held before the
+ * call.  Row r has outer * pieces pieces, at data + o * outer_stride + r * row_stride + p * piece_stride (strides in bytes), each
+ * of `positions` positions of position_bytes bytes one behind the other: [layers, rows, heads, positions, width] has outer =
+ * layers and pieces = heads, [layers, rows, positions, heads, width] outer = layers, pieces = 1 and position_bytes of all heads.
+ * begin_dev, end_dev (device, G int32 each, may be NULL: 0 and positions): only positions begin[g] <= t < end[g] of group g's
+ * rows are touched (its beams have the prompt in common); values outside 0 .. positions count as these.  Pieces must not
+ * overlap.  parents_dev: device, G * K int32, each in its row's group; rows with -1, or any row outside the group, stay.    */
+int32_t xg2_beam_reorder_rows(void* data_dev, int32_t groups, int32_t beams, const int32_t* parents_dev, int64_t row_stride,
+                              int32_t outer, int64_t outer_stride, int32_t pieces, int64_t piece_stride, int32_t positions,
+                              int64_t position_bytes, const int32_t* begin_dev, const int32_t* end_dev, void* hip_stream);
+
+/* The sequences of all beams after `steps` steps: tokens_dev and parents_dev hold what the steps chose, step t at t * step_stride
+ * (G * K int32 each).  Row r of out_tokens_dev (out_stride int32 from one to the next) receives steps tokens: that of row r at the
+ * last step, of its parent at the step before, and so on.  Where the way leaves the group (a parent of -1, or any outside) the
+ * steps before are -1.  out_lengths_dev (may be NULL): per row, steps up to and with the last token that is not negative.    */
+int32_t xg2_beam_backtrace(const int32_t* tokens_dev, const int32_t* parents_dev, int32_t steps, int64_t step_stride, int32_t groups,
+                           int32_t beams, int32_t* out_tokens_dev, int64_t out_stride, int32_t* out_lengths_dev, void* hip_stream);
 
 #ifdef __cplusplus
 }

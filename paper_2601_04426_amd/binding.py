@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libxg2mask.so")
 
 XG2_OK, XG2_EINVAL, XG2_EPARSE, XG2_EREJECTED, XG2_EOVERFLOW, XG2_EHIP = 0, -1, -2, -3, -4, -5
 XG2_F32, XG2_BF16 = 0, 1
+XG2_OVER_ALLOWED, XG2_OVER_ALL = 0, 1
 
 EXPORTS = [
     "xg2_last_error", "xg2_vocab_create", "xg2_vocab_destroy", "xg2_grammar_create", "xg2_grammar_destroy",
@@ -29,6 +30,7 @@ EXPORTS = [
     "xg2_fill_last_device_us", "xg2_fill_last_status", "xg2_fill_last_recheck_tokens",
     "xg2_apply_token_bitmask", "xg2_batch_create", "xg2_batch_destroy", "xg2_batch_assign", "xg2_batch_accept_tokens",
     "xg2_batch_fill_next_token_bitmask", "xg2_batch_row_info",
+    "xg2_beam_select_workspace", "xg2_beam_select", "xg2_batch_reorder", "xg2_beam_reorder_rows", "xg2_beam_backtrace",
 ]
 
 
@@ -111,6 +113,11 @@ def _load() -> ctypes.CDLL:
     L.xg2_batch_accept_tokens.argtypes = [vp, vp, vp, vp]
     L.xg2_batch_fill_next_token_bitmask.argtypes = [vp, vp, i64, vp]
     L.xg2_batch_row_info.argtypes = [vp, i32, vp]
+    L.xg2_beam_select_workspace.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+    L.xg2_beam_select.argtypes = [vp, i32, i32, i32, i32, i64, vp, i64, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.xg2_batch_reorder.argtypes = [vp, i32, vp, vp, vp]
+    L.xg2_beam_reorder_rows.argtypes = [vp, i32, i32, vp, i64, i32, i64, i32, i64, i32, i64, vp, vp, vp]
+    L.xg2_beam_backtrace.argtypes = [vp, vp, i32, i64, i32, i32, vp, i64, vp, vp]
     for name in EXPORTS:
         if name not in ("xg2_last_error",) and not name.endswith("_destroy"):
             getattr(L, name).restype = i32
@@ -337,6 +344,10 @@ class DeviceBatch:
     def fill_next_token_bitmask(self, bitmask_ptr: int, row_stride_words: int, stream: int = 0) -> None:
         _check(lib.xg2_batch_fill_next_token_bitmask(self.h, ctypes.c_void_p(bitmask_ptr), row_stride_words, ctypes.c_void_p(stream)))
 
+    def reorder(self, beams: int, parents_ptr: int, status_ptr: int = 0, stream: int = 0) -> None:
+        """Slot b takes over the state of slot parents[b] (-1: keeps its own); parents lie within their group of `beams` slots."""
+        _check(lib.xg2_batch_reorder(self.h, beams, parents_ptr, status_ptr or None, stream))
+
     def row_info(self, row: int) -> dict:
         out = np.zeros(8, dtype=np.int32)
         _check(lib.xg2_batch_row_info(self.h, row, out.ctypes.data))
@@ -410,3 +421,34 @@ def apply_token_bitmask(logits_ptr: int, dtype: int, B: int, V: int, row_stride_
                         bm_row_stride_words: int, stream: int = 0) -> None:
     _check(lib.xg2_apply_token_bitmask(ctypes.c_void_p(logits_ptr), dtype, B, V, row_stride_elems,
                                        ctypes.c_void_p(bitmask_ptr), bm_row_stride_words, ctypes.c_void_p(stream)))
+
+
+def beam_select_workspace(dtype: int, groups: int, beams: int, V: int, n_out: int) -> int:
+    """Bytes of workspace that beam_select needs."""
+    n = ctypes.c_size_t(0)
+    _check(lib.xg2_beam_select_workspace(dtype, groups, beams, V, n_out, ctypes.byref(n)))
+    return n.value
+
+
+def beam_select(logits_ptr: int, dtype: int, groups: int, beams: int, V: int, row_stride_elems: int, scores_ptr: int, n_out: int,
+                out_scores_ptr: int, out_parents_ptr: int, out_tokens_ptr: int, workspace_ptr: int, workspace_bytes: int,
+                bitmask_ptr: int = 0, bm_row_stride_words: int = 0, over: int = XG2_OVER_ALLOWED, finished_ptr: int = 0, eos_id: int = -1,
+                out_finished_ptr: int = 0, stream: int = 0) -> None:
+    """The best n_out candidates of every group of beams: scores, parents (rows), tokens and whether they have ended."""
+    _check(lib.xg2_beam_select(logits_ptr, dtype, groups, beams, V, row_stride_elems, bitmask_ptr or None, bm_row_stride_words, over, scores_ptr,
+                               finished_ptr or None, eos_id, n_out, out_scores_ptr, out_parents_ptr, out_tokens_ptr, out_finished_ptr or None,
+                               workspace_ptr, workspace_bytes, stream))
+
+
+def beam_reorder_rows(data_ptr: int, groups: int, beams: int, parents_ptr: int, row_stride: int, positions: int, position_bytes: int,
+                      outer: int = 1, outer_stride: int = 0, pieces: int = 1, piece_stride: int = 0, begin_ptr: int = 0, end_ptr: int = 0,
+                      stream: int = 0) -> None:
+    """In place: the beams' rows of a buffer take over what their parents' rows held (strides in bytes)."""
+    _check(lib.xg2_beam_reorder_rows(data_ptr, groups, beams, parents_ptr, row_stride, outer, outer_stride, pieces, piece_stride, positions,
+                                     position_bytes, begin_ptr or None, end_ptr or None, stream))
+
+
+def beam_backtrace(tokens_ptr: int, parents_ptr: int, steps: int, step_stride: int, groups: int, beams: int, out_ptr: int, out_stride: int,
+                   lengths_ptr: int = 0, stream: int = 0) -> None:
+    """The sequences of all beams from the steps' tokens and parents."""
+    _check(lib.xg2_beam_backtrace(tokens_ptr, parents_ptr, steps, step_stride, groups, beams, out_ptr, out_stride, lengths_ptr or None, stream))

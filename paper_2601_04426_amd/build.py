@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libxg2mask.so")
-SOURCES = ["grammar.cpp", "tables.cpp", "api.cpp", "kernels.hip"]
+SOURCES = ["grammar.cpp", "tables.cpp", "api.cpp", "kernels.hip", "beam.cpp", "beam.hip"]
 ARCH = "gfx950"
 
 

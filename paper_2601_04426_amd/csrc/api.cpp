@@ -24,6 +24,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "beam.hpp"
 #include "block_list.hpp"
 #include "device.hpp"
 #include "flat_map.hpp"
@@ -2706,3 +2707,15 @@ int32_t xg2_batch_row_info(xg2_batch* batch, int32_t row, int32_t* info_host) {
 }
 
 }  // extern "C"
+
+// ---- what beam.cpp works with ---------------------------------------------------------------------------------------
+namespace xg2 {
+int32_t api_fail(int32_t code, const char* message) { return fail(code, message); }
+int32_t api_guarded(int32_t (*call)(void*), void* arg) { return guarded([&]() -> int32_t { return call(arg); }); }
+void api_require_device() { require_device(); }
+BatchView api_batch(xg2_batch* batch) {
+    BatchImpl& b = *batch->p;
+    std::unique_lock<std::mutex> lock(b.mu);
+    return {std::move(lock), b.d, b.n_assigned == b.B};
+}
+}  // namespace xg2
