@@ -25,7 +25,7 @@ struct Shape { size_t stats, blocks; uint32_t pieces; };
 Shape select_shape(int32_t dtype, int32_t groups, int32_t beams, int32_t V) {
     const size_t rows = (size_t)groups * (size_t)beams;
     const uint32_t pieces = beam_pieces(V, dtype == XG2_F32 ? 4 : 2);
-    return {rounded(rows * pieces * sizeof(float2)), rounded(rows * pieces * kBeamPieceBlocks * sizeof(float)), pieces};
+    return {rounded(rows * pieces * sizeof(float4)), rounded(rows * pieces * kBeamPieceBlocks * sizeof(float)), pieces};
 }
 const char* bad_shape(int32_t dtype, int32_t groups, int32_t beams, int32_t V, int32_t n_out) {
     if (dtype != XG2_F32 && dtype != XG2_BF16) return "unknown dtype";
@@ -73,7 +73,7 @@ int32_t xg2_beam_select(const void* logits_dev, int32_t dtype, int32_t groups, i
         A.logits = logits_dev; A.row_stride = row_stride_elems;
         A.bitmask = reinterpret_cast<const uint32_t*>(bitmask_dev); A.bm_stride = bm_row_stride_words;
         A.scores = scores_dev; A.finished = finished_dev;
-        A.stats = static_cast<float2*>(workspace_dev);
+        A.stats = static_cast<float4*>(workspace_dev);
         A.block_max = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + s.stats);
         A.out_scores = out_scores_dev; A.out_parents = out_parents_dev; A.out_tokens = out_tokens_dev; A.out_finished = out_finished_dev;
         A.groups = (uint32_t)groups; A.beams = (uint32_t)beams; A.n_out = (uint32_t)n_out; A.pieces = s.pieces;

@@ -13,7 +13,56 @@ namespace {
 
 constexpr float NINF = -__builtin_inff();
 
+// Memory that is known to be device memory: a pointer out of a struct of arguments could be of any kind, and loads of that sort are waited
+// for together with those of LDS.
+#if defined(__HIP_DEVICE_COMPILE__)
+#define XG2_GLOBAL __attribute__((address_space(1)))
+#else
+#define XG2_GLOBAL
+#endif
+template <class P> using Global = XG2_GLOBAL P*;
+
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ float lane_float(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+
+// Sums and maxima over lanes: the partners within a row of 16 lanes, then the rows.  After the first four steps all lanes of a row have
+// the row's value, after the next (lane 15 of a row to the row behind it) lanes 31 and 63 that of 32 lanes, after the last lane 63 that of all.
+constexpr int DPP_SWAP1 = 0xB1, DPP_SWAP2 = 0x4E, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140, DPP_ROW_BCAST15 = 0x142, DPP_ROW_BCAST31 = 0x143;
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ float moved(float own, float v) { return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(own), __float_as_int(v), CTRL, ROWS, 0xF, false)); }
+// The larger of two (three) numbers, of two with a quiet NaN the other.  (fmaxf would take an instruction more for each operand that came
+// from memory, to make signalling NaN quiet ones; where one of these is met the sum of exponentials is NaN, which is looked for.)
+__device__ __forceinline__ float larger(float a, float b) { float d; asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b)); return d; }
+__device__ __forceinline__ float larger(float a, float b, float c) { float d; asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c)); return d; }
+#if defined(__HIP_DEVICE_COMPILE__)
+#define READABLE(v) asm volatile("s_nop 1" : "+v"(v))                // what inline assembly wrote, before another lane reads it
+#else
+#define READABLE(v) (void)0
+#endif
+// Four values at a time, stage by stage, so that none is read across lanes within two instructions of being written (which the device does
+// not wait for, and of which the compiler knows nothing here).
+#if defined(__HIP_DEVICE_COMPILE__)
+#define XG2_MAX4(HOW) "v_max_f32_dpp %0, %0, %0 " HOW "\n\tv_max_f32_dpp %1, %1, %1 " HOW "\n\tv_max_f32_dpp %2, %2, %2 " HOW "\n\tv_max_f32_dpp %3, %3, %3 " HOW "\n\t"
+#define XG2_MAX4_16 "s_nop 1\n\t" XG2_MAX4("quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf") XG2_MAX4("quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf") \
+    XG2_MAX4("row_half_mirror row_mask:0xf bank_mask:0xf") XG2_MAX4("row_mirror row_mask:0xf bank_mask:0xf")
+__device__ __forceinline__ void largest_of_32(float& a, float& b, float& c, float& d) {                                                     // lanes 31, 63
+    asm volatile(XG2_MAX4_16 XG2_MAX4("row_bcast:15 row_mask:0xa bank_mask:0xf") "s_nop 1" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+}
+__device__ __forceinline__ void largest_of_64(float& a, float& b, float& c, float& d) {                                                     // lane 63
+    asm volatile(XG2_MAX4_16 XG2_MAX4("row_bcast:15 row_mask:0xa bank_mask:0xf") XG2_MAX4("row_bcast:31 row_mask:0xc bank_mask:0xf") "s_nop 1" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+}
+#else
+__device__ void largest_of_32(float&, float&, float&, float&) {}
+__device__ void largest_of_64(float&, float&, float&, float&) {}
+#endif
+__device__ __forceinline__ float sum_of_64(float v) {                                                                                      // lane 63
+    v += moved<DPP_SWAP1>(v, v);
+    v += moved<DPP_SWAP2>(v, v);
+    v += moved<DPP_HALF_MIRROR>(v, v);
+    v += moved<DPP_MIRROR>(v, v);
+    v += moved<DPP_ROW_BCAST15, 0xA>(0.f, v);
+    return v + moved<DPP_ROW_BCAST31, 0xC>(0.f, v);
+}
 
 // ---- selection ------------------------------------------------------------------------------------------------------
 // score(row, token) = s_row - L_row + x, L_row = log of the sum of exp x over the tokens that count.  Chosen are the n best of all rows
@@ -25,24 +74,33 @@ constexpr int kScanWaves = 4;
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr double LN2 = 0.693147180559945309417232;
 
+typedef uint32_t Vec4 __attribute__((ext_vector_type(4)));
 template <class E> struct Elem;
 template <> struct Elem<float> {
     static constexpr int EPV = 4;
-    static __device__ __forceinline__ float value(float e) { return e; }
-    static __device__ __forceinline__ void unpack(const uint4& v, float* x) { x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w); }
+    static __device__ __forceinline__ float load(const float* p) { return *(Global<const float>)p; }
+    static __device__ __forceinline__ void unpack(const Vec4& v, float* x) { _Pragma("unroll") for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(v[k]); }
+    // the vector at element e of the row, put together; what is not of the row is any of its logits
+    static __device__ __forceinline__ Vec4 gather(const float* row, int e, int V) {
+        Vec4 v;
+        _Pragma("unroll") for (int k = 0; k < 4; ++k) v[k] = __float_as_uint(load(row + min(max(e + k, 0), V - 1)));
+        return v;
+    }
 };
-struct Bf16 { uint16_t bits; };
-template <> struct Elem<Bf16> {
+template <> struct Elem<uint16_t> {                                  // bfloat16
     static constexpr int EPV = 8;
-    static __device__ __forceinline__ float value(Bf16 e) { return __uint_as_float((uint32_t)e.bits << 16); }
-    static __device__ __forceinline__ void unpack(const uint4& v, float* x) {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        _Pragma("unroll") for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+    static __device__ __forceinline__ float load(const uint16_t* p) { return __uint_as_float((uint32_t)*(Global<const uint16_t>)p << 16); }
+    static __device__ __forceinline__ void unpack(const Vec4& v, float* x) {
+        _Pragma("unroll") for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(v[k] << 16); x[2 * k + 1] = __uint_as_float(v[k] & 0xFFFF0000u); }
+    }
+    static __device__ __forceinline__ Vec4 gather(const uint16_t* row, int e, int V) {
+        uint32_t x[8];
+        _Pragma("unroll") for (int k = 0; k < 8; ++k) x[k] = *(Global<const uint16_t>)(row + min(max(e + k, 0), V - 1));
+        return Vec4{x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16};
     }
 };
 
-// The larger of two numbers; a NaN loses.
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ Vec4 stats_of(float top, float sum, float best) { return Vec4{__float_as_uint(top), __float_as_uint(sum), __float_as_uint(best), 0u}; }
 
 // Elements of a row before the 128-byte boundary that its pieces and blocks are counted from.
 template <class E> __device__ __forceinline__ int before_row(const E* row) { return (int)(reinterpret_cast<uintptr_t>(row) & 127) / (int)sizeof(E); }
@@ -56,16 +114,15 @@ __device__ __forceinline__ bool live_row(const BeamSelect& A, uint32_t r) {
 // WHICH: 0 no mask, 1 the softmax goes over the allowed tokens, 2 over all.
 template <class E, int WHICH>
 __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(BeamSelect A, uint32_t first_row) {
-    constexpr int EPV = Elem<E>::EPV, STEPS = kBeamPiece / 64 / EPV, LANES = kBeamBlock / EPV;   // lanes that share a block
+    constexpr int EPV = Elem<E>::EPV, STEPS = kBeamPiece / 64 / EPV, VPW = 32 / EPV;   // vectors of a mask word
     constexpr uint32_t ALL = (1u << EPV) - 1;
-    const uint32_t r = first_row + blockIdx.y, lane = threadIdx.x & 63, piece = blockIdx.x * kScanWaves + uniform(threadIdx.x >> 6);
+    const uint32_t r = first_row + blockIdx.y, lane = threadIdx.x & 63, piece = blockIdx.x * (blockDim.x >> 6) + uniform(threadIdx.x >> 6);
     if (piece >= A.pieces || !live_row(A, r)) return;
     const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
-    const int V = A.V;
-    const long long e0 = (long long)piece * kBeamPiece - before_row(row);
+    const int V = A.V, e0 = (int)piece * kBeamPiece - before_row(row);             // (V is at most 2^30)
     const bool inner = e0 >= 0 && e0 + kBeamPiece <= V;
     // this lane's 32 tokens from e0 + 32 * lane on: which are in the row, and which of them are allowed
-    const long long first = e0 + 32 * (long long)lane;
+    const int first = e0 + 32 * (int)lane;
     uint32_t inside = ~0u;
     if (!inner) {
         if (first < 0) inside = first <= -32 ? 0 : ~0u << -first;
@@ -73,9 +130,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(BeamSelect A, uin
     }
     uint32_t allowed = inside;
     if (WHICH != 0) {
-        const uint32_t* const bm = A.bitmask + (long long)r * A.bm_stride;
-        const long long at = first >> 5, last = (V - 1) >> 5;       // (an arithmetic shift: rounds down)
-        const int shift = (int)(e0 & 31);                            // (the same in all lanes)
+        const Global<const uint32_t> bm = (Global<const uint32_t>)(A.bitmask + (long long)r * A.bm_stride);
+        const int at = first >> 5, last = (V - 1) >> 5, shift = e0 & 31;            // (an arithmetic shift: rounds down; shift is the same in all lanes)
         uint32_t word = at >= 0 && at <= last ? bm[at] : 0;
         if (shift != 0) {
             const uint32_t next = at + 1 >= 0 && at + 1 <= last ? bm[at + 1] : 0;
@@ -84,393 +140,523 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(BeamSelect A, uin
         allowed &= word;
     }
     const uint32_t counted = WHICH == 1 ? allowed : inside;
-    float2* const stats = A.stats + ((size_t)r * A.pieces + piece);
-    float* const block_max = A.block_max + ((size_t)r * A.pieces + piece) * kBeamPieceBlocks;
+    const Global<Vec4> stats = (Global<Vec4>)(A.stats + ((size_t)r * A.pieces + piece));
+    const Global<float> block_max = (Global<float>)(A.block_max + ((size_t)r * A.pieces + piece) * kBeamPieceBlocks);
     if (WHICH == 1 && __ballot(counted != 0) == 0) {
-        if (lane == 0) *stats = make_float2(NINF, 0.f);
+        if (lane == 0) *stats = stats_of(NINF, 0.f, NINF);
         if (lane < kBeamPieceBlocks) block_max[lane] = NINF;
         return;
     }
     const E* const from = row + e0;
-    uint4 raw[STEPS];
+    const Global<const Vec4> vectors = (Global<const Vec4>)from;
+    Vec4 raw[STEPS];
     uint32_t bits[STEPS];
-#pragma unroll
-    for (int j = 0; j < STEPS; ++j) {
-        const int v = j * 64 + (int)lane;
-        bits[j] = ((uint32_t)__shfl((int)counted, v / (32 / EPV)) >> (v % (32 / EPV) * EPV)) & ALL;
-        raw[j] = make_uint4(0, 0, 0, 0);
-        const long long e = e0 + v * EPV;
-        if (bits[j] != 0) {
-            if (e >= 0 && e + EPV <= V) raw[j] = reinterpret_cast<const uint4*>(from)[v];
-            else {                                                   // a vector that the row shares with its neighbours
-                E part[EPV] = {};
-                for (int c = 0; c < EPV; ++c) if (e + c >= 0 && e + c < V) part[c] = row[e + c];
-                __builtin_memcpy(&raw[j], part, 16);
+    if (WHICH != 1 && inner) {
+        _Pragma("unroll") for (int j = 0; j < STEPS; ++j) { bits[j] = ALL; raw[j] = vectors[j * 64 + (int)lane]; }
+    } else {
+        _Pragma("unroll") for (int j = 0; j < STEPS; ++j) bits[j] = ((uint32_t)__shfl((int)counted, (j * 64 + (int)lane) / VPW) >> ((int)lane % VPW * EPV)) & ALL;
+        // A vector that the row shares with its neighbours lies between the buffer's first and last logit all the same, but for one at the
+        // begin of the first row and one at the end of the last: these are put together from logits.
+        const long long at = (long long)r * A.row_stride + e0, end = (long long)(A.groups * A.beams - 1) * A.row_stride + V;
+        const bool apart = !inner && (at < 0 || at + kBeamPiece > end);
+        unsigned long long open = 0;
+        _Pragma("unroll") for (int j = 0; j < STEPS; ++j) {
+            const int v = j * 64 + (int)lane;
+            const bool whole = !apart || (at + v * EPV >= 0 && at + (v + 1) * EPV <= end);
+            raw[j] = Vec4{0, 0, 0, 0};
+            if (bits[j] != 0 && whole) raw[j] = vectors[v];
+            if (apart) open |= __ballot(bits[j] != 0 && !whole);
+        }
+        if (open != 0) {
+            _Pragma("unroll") for (int j = 0; j < STEPS; ++j) {
+                const int v = j * 64 + (int)lane;
+                if (bits[j] != 0 && !(at + v * EPV >= 0 && at + (v + 1) * EPV <= end)) raw[j] = Elem<E>::gather(row, e0 + v * EPV, V);
             }
         }
     }
-    float x[STEPS][EPV], top = NINF;
+    float x[STEPS][EPV], top = NINF, best[STEPS];
 #pragma unroll
     for (int j = 0; j < STEPS; ++j) {
         Elem<E>::unpack(raw[j], x[j]);
-        _Pragma("unroll") for (int c = 0; c < EPV; ++c) if (!((bits[j] >> c) & 1)) x[j][c] = NINF;
-        float m = NINF, best;
-        _Pragma("unroll") for (int c = 0; c < EPV; ++c) m = larger(m, x[j][c]);
-        top = larger(top, m);
-        best = m;
-        if (WHICH == 2) {
-            const int v = j * 64 + (int)lane;
-            const uint32_t ok = ((uint32_t)__shfl((int)allowed, v / (32 / EPV)) >> (v % (32 / EPV) * EPV)) & ALL;
-            best = NINF;
-            _Pragma("unroll") for (int c = 0; c < EPV; ++c) best = larger(best, (ok >> c) & 1 ? x[j][c] : NINF);
+        if (WHICH == 1 || !inner) {
+            // (a bit spread over a word picks the logit or minus infinity)
+            _Pragma("unroll") for (int c = 0; c < EPV; ++c) {
+                const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)bits[j], c, 1);
+                x[j][c] = __uint_as_float((__float_as_uint(x[j][c]) & m) | (__float_as_uint(NINF) & ~m));
+            }
         }
-        _Pragma("unroll") for (int d = 1; d < LANES; d *= 2) best = larger(best, __shfl_xor(best, d));
-        if (lane % LANES == 0) block_max[j * (64 / LANES) + (int)lane / LANES] = best;
+        float m = larger(x[j][0], x[j][1], x[j][2]);
+        if (EPV == 8) { m = larger(m, x[j][3], x[j][4]); m = larger(m, x[j][5], x[j][6]); }
+        m = larger(m, x[j][EPV - 1]);
+        top = larger(top, m);
+        if (WHICH == 2) {
+            const uint32_t ok = (uint32_t)__shfl((int)allowed, (j * 64 + (int)lane) / VPW) >> ((int)lane % VPW * EPV);
+            float y[EPV];
+            _Pragma("unroll") for (int c = 0; c < EPV; ++c) {
+                const uint32_t w = (uint32_t)__builtin_amdgcn_sbfe((int)ok, c, 1);
+                y[c] = __uint_as_float((__float_as_uint(x[j][c]) & w) | (__float_as_uint(NINF) & ~w));
+            }
+            m = larger(y[0], y[1], y[2]);
+            if (EPV == 8) { m = larger(m, y[3], y[4]); m = larger(m, y[5], y[6]); }
+            m = larger(m, y[EPV - 1]);
+        }
+        best[j] = m;
     }
-    _Pragma("unroll") for (int d = 1; d < 64; d *= 2) top = larger(top, __shfl_xor(top, d));
+    if (EPV == 8) largest_of_32(best[0], best[1], best[2], best[3]);
+    else { _Pragma("unroll") for (int j = 0; j < STEPS; j += 4) largest_of_64(best[j], best[j + 1], best[j + 2], best[j + 3]); }
+    // the piece's largest allowed logit, and its largest that counts
+    float ok_max = best[0];
+    _Pragma("unroll") for (int j = 1; j < STEPS; ++j) ok_max = larger(ok_max, best[j]);
+    READABLE(ok_max);
+    ok_max = EPV == 8 ? larger(lane_float(ok_max, 31), lane_float(ok_max, 63)) : lane_float(ok_max, 63);
+    float all = ok_max;
+    if (WHICH == 2) {
+        float same = top, same2 = top, same3 = top;
+        largest_of_64(top, same, same2, same3);
+        all = lane_float(top, 63);
+    }
+    if (EPV == 8) {
+        if ((lane & 31) == 31) { _Pragma("unroll") for (int j = 0; j < STEPS; ++j) block_max[2 * j + (lane >> 5)] = best[j]; }
+    } else if (lane == 63) {
+        Vec4 b[2];
+        _Pragma("unroll") for (int j = 0; j < STEPS; ++j) b[j / 4][j % 4] = __float_as_uint(best[j]);
+        ((Global<Vec4>)block_max)[0] = b[0];
+        ((Global<Vec4>)block_max)[1] = b[1];
+    }
     float sum = 0;
-    if (top > NINF) {
-        const float c = __fmul_rn(top, LOG2E);
+    if (all > NINF) {
+        const float c = larger(__fmul_rn(all, LOG2E), -3.4028234e38f);             // (finite, or minus infinity would come back as NaN)
         // (added up as a tree: 11 additions between a term and the sum, which is what its error is derived from)
         float part[STEPS * EPV];
         _Pragma("unroll") for (int i = 0; i < STEPS * EPV; ++i) part[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i / EPV][i % EPV], LOG2E, -c));
         _Pragma("unroll") for (int d = STEPS * EPV / 2; d > 0; d /= 2)
             _Pragma("unroll") for (int i = 0; i < d; ++i) part[i] += part[i + d];
-        sum = part[0];
-        _Pragma("unroll") for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        sum = sum_of_64(part[0]);
     }
-    if (lane == 0) *stats = make_float2(top, sum);
+    if (lane == 63) *stats = stats_of(all, sum, ok_max);
 }
 
 // ---- the best candidates of a group ---------------------------------------------------------------------------------
 // One workgroup per group.  How near a score is to the best is measured in bins whose width grows with the distance (64 to an octave
-// from 2^-6 on), so that one count over the blocks' best scores gives a line that at least n of them lie above and few more.
-constexpr int kPickThreads = 1024, kPickBins = 1024, kPickBlocks = 1024, kPickElems = 2048;
+// from 2^-6 on).  A count of the pieces' best scores gives the bin that the n-th best of them lies in: at least n candidates lie in it or
+// below, so only pieces, in them blocks, in them tokens that do are looked at, which are few more than n.  16 lanes have a row's pieces.
+constexpr int kPickThreads = 1024, kPickMostWaves = kPickThreads / 64, kPickBins = 1024, kPickListed = 1024, kPickElems = 2048, kPickHeld = 5;
+
+constexpr uint32_t kRowShift = 26, kRowBits = (1u << kRowShift) - 1;
+static_assert(kBeamsMost <= 1u << (32 - kRowShift) && ((uint64_t)kBeamVocabMost + 64 + kBeamPiece) / kBeamBlock <= kRowBits, "a row and its block fit a word");
+
 enum RowState : uint32_t { ROW_NONE, ROW_LIVE, ROW_ENDED };
+// A candidate: its score and its place in the order of rows and tokens, row << 32 | token + 1.
+struct alignas(16) Candidate { double score; uint64_t at; };
 struct PickShared {
     double base[kBeamsMost];                   // score of a token of the row: base + its logit (infinite: base, where the logit is +inf)
     uint32_t state[kBeamsMost];
     uint32_t infinite[kBeamsMost], exact[kBeamsMost], repair[kBeamsMost];
-    double near_top[kPickThreads / 64];
-    uint32_t bins[kPickBins];
-    uint32_t blocks[kPickBlocks];              // row in the group * blocks of a row + block
-    uint32_t n_blocks, n_elems, last_bin, any, found;
-    double score[kPickElems];
+    double wave_top[kPickMostWaves];
+    uint32_t bins[kPickBins];                  // bin b at (b % 16) * 64 + b / 16
+    uint32_t pieces[kPickListed];              // row in the group << kRowShift | piece
+    uint32_t blocks[kPickListed];              // row in the group << kRowShift | block
+    uint32_t n_pieces, n_blocks, n_elems;
+    Candidate found[kPickElems];
     float x[kPickElems];
-    int32_t token[kPickElems];
-    uint16_t row[kPickElems];
+    uint32_t place[kPickElems];
     uint16_t sorted[kPickElems];
-    double r_score[kPickThreads / 64];
-    uint32_t r_row[kPickThreads / 64];
-    long long r_at[kPickThreads / 64];
+    Candidate wave_best[kPickMostWaves];
 };
+
+// 2^t (down to -1000), and the natural logarithm of a sum of at least a half, to some 13 digits (what is added up has seven).
+__device__ __forceinline__ double exp2_of(double t) {
+    const double n = __builtin_rint(t), f = (t - n) * LN2;
+    double p = 1.0 / 3628800;
+    constexpr double C[] = {1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 1.0 / 2, 1.0, 1.0};
+    _Pragma("unroll") for (int i = 0; i < 10; ++i) p = __builtin_fma(p, f, C[i]);
+    return __builtin_ldexp(p, (int)n);
+}
+__device__ __forceinline__ double log_of(double v) {
+    const double y = (double)__builtin_amdgcn_logf((float)v), e = v * exp2_of(-y) - 1.0;      // (log2 in 32 bits, then what is missing)
+    return y * LN2 + e - e * e * 0.5;
+}
+// Over a row of 16 lanes, in all of them; and how many of the lanes' counts lie up to and with a lane.
+template <int CTRL>
+__device__ __forceinline__ double moved(double v) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp((int)u, (int)u, CTRL, 0xF, 0xF, false), hi = (uint32_t)__builtin_amdgcn_update_dpp((int)(u >> 32), (int)(u >> 32), CTRL, 0xF, 0xF, false);
+    return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+__device__ __forceinline__ double sum_of_16(double v) {
+    v += moved<DPP_SWAP1>(v);
+    v += moved<DPP_SWAP2>(v);
+    v += moved<DPP_HALF_MIRROR>(v);
+    return v + moved<DPP_MIRROR>(v);
+}
+__device__ __forceinline__ float largest_of_16(float v) {
+    v = fmaxf(v, moved<DPP_SWAP1>(v, v));
+    v = fmaxf(v, moved<DPP_SWAP2>(v, v));
+    v = fmaxf(v, moved<DPP_HALF_MIRROR>(v, v));
+    return fmaxf(v, moved<DPP_MIRROR>(v, v));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t shifted(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ uint32_t count_upto(uint32_t v) {
+    v += shifted<0x111, 0xF>(v);                                     // from 1, 2, 4 and 8 lanes below in the row
+    v += shifted<0x112, 0xF>(v);
+    v += shifted<0x114, 0xF>(v);
+    v += shifted<0x118, 0xF>(v);
+    v += shifted<DPP_ROW_BCAST15, 0xA>(v);
+    return v + shifted<DPP_ROW_BCAST31, 0xC>(v);
+}
 
 __device__ __forceinline__ uint32_t bin_of(double top, double score) {
     const float d = (float)(top - score) + 0.015625f;                // (monotone: each step rounds one way for all)
     const uint32_t b = (__float_as_uint(d) >> 17) - (__float_as_uint(0.015625f) >> 17);
     return b < kPickBins - 1 ? b : kPickBins - 1;
 }
+// How far from the best the last score of a bin may lie (a bound).
+__device__ __forceinline__ double reach_of(uint32_t bin) { return (double)__uint_as_float((bin + 1 + (__float_as_uint(0.015625f) >> 17)) << 17); }
+__device__ __forceinline__ uint32_t bin_at(uint32_t b) { return b % 16 * 64 + b / 16; }
 __device__ __forceinline__ double score_of(const PickShared& S, uint32_t k, float x) {
     return S.base[k] + (double)(S.infinite[k] ? (x == -NINF ? 0.f : NINF) : x);
 }
 __device__ __forceinline__ bool token_allowed(const BeamSelect& A, uint32_t r, long long t) {
-    return !A.bitmask || ((A.bitmask[(long long)r * A.bm_stride + (t >> 5)] >> (t & 31)) & 1u);
+    return !A.bitmask || ((((Global<const uint32_t>)A.bitmask)[(long long)r * A.bm_stride + (t >> 5)] >> (t & 31)) & 1u);
 }
+__device__ __forceinline__ uint64_t place_of(uint32_t row, long long token) { return (uint64_t)row << 32 | (uint64_t)(token + 1); }
+__device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) { return a.score > b.score || (a.score == b.score && a.at < b.at); }
 
-// The row's sum in 64 bits, and its blocks' maxima without NaN: what the first kernel left of the row is not used.
+// The row's sum in 64 bits, and the maxima of its pieces and blocks without NaN: what the first kernel left of the row is not used.
 template <class E>
-__device__ void repair_row(const BeamSelect& A, PickShared& S, uint32_t g, uint32_t k) {
-    const uint32_t r = g * A.beams + k, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_blocks = A.pieces * kBeamPieceBlocks;
+__device__ __attribute__((noinline)) void repair_row(const BeamSelect& A, PickShared& S, uint32_t g, uint32_t k) {
+    const uint32_t r = g * A.beams + k, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x >> 6;
     const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
-    const int before = before_row(row);
-    float* const block_max = A.block_max + (size_t)r * n_blocks;
     float top = NINF;
-    __syncthreads();                                                 // (S.near_top has been read by all)
-    for (uint32_t b = wave; b < n_blocks; b += kPickThreads / 64) {
-        float best = NINF;
-        for (int c = 0; c < kBeamBlock; c += 64) {
-            const long long t = (long long)b * kBeamBlock - before + c + lane;
-            if (t < 0 || t >= A.V) continue;
-            const float x = Elem<E>::value(row[t]);
-            const bool ok = token_allowed(A, r, t);
-            if (x != x) continue;
-            if (ok) best = x > best ? x : best;
-            if (ok || A.over_all) top = x > top ? x : top;
+    __syncthreads();                                                 // (S.wave_top has been read by all)
+    for (uint32_t p = wave; p < A.pieces; p += waves) {
+        float piece_best = NINF;
+        for (int b = 0; b < kBeamPieceBlocks; ++b) {
+            const int t0 = (int)p * kBeamPiece + b * kBeamBlock - before_row(row);
+            float best = NINF;
+            for (int c = 0; c < kBeamBlock; c += 64) {
+                const int t = t0 + c + (int)lane;
+                if (t < 0 || t >= A.V) continue;
+                const float x = Elem<E>::load(row + t);
+                const bool ok = token_allowed(A, r, t);
+                if (ok) best = x > best ? x : best;                  // (false for NaN)
+                if (ok || A.over_all) top = x > top ? x : top;
+            }
+            for (int d = 1; d < 64; d *= 2) { const float o = __shfl_xor(best, d); best = o > best ? o : best; }
+            if (lane == 0) ((Global<float>)A.block_max)[((size_t)r * A.pieces + p) * kBeamPieceBlocks + b] = best;
+            piece_best = best > piece_best ? best : piece_best;
         }
-        for (int d = 1; d < 64; d *= 2) { const float o = __shfl_xor(best, d); best = o > best ? o : best; }
-        if (lane == 0) block_max[b] = best;
+        if (lane == 0) ((Global<float>)(A.stats + ((size_t)r * A.pieces + p)))[2] = piece_best;
     }
     for (int d = 1; d < 64; d *= 2) { const float o = __shfl_xor(top, d); top = o > top ? o : top; }
-    if (lane == 0) S.near_top[wave] = top;
+    if (lane == 0) S.wave_top[wave] = top;
     __syncthreads();
-    for (int w = 0; w < kPickThreads / 64; ++w) top = (float)S.near_top[w] > top ? (float)S.near_top[w] : top;
+    for (uint32_t w = 0; w < waves; ++w) top = (float)S.wave_top[w] > top ? (float)S.wave_top[w] : top;
     __syncthreads();
     double sum = 0;
-    for (long long t = tid; t < A.V; t += kPickThreads) {
-        const float x = Elem<E>::value(row[t]);
-        if (x != x || x == NINF || !(A.over_all || token_allowed(A, r, t))) continue;
+    for (int t = (int)tid; t < A.V; t += (int)blockDim.x) {
+        const float x = Elem<E>::load(row + t);
+        if (!(x > NINF) || !(A.over_all || token_allowed(A, r, t))) continue;
         if (top == -NINF) sum += x == top ? 1.0 : 0.0;
         else sum += exp((double)x - (double)top);
     }
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    if (lane == 0) S.near_top[wave] = sum;
+    if (lane == 0) S.wave_top[wave] = sum;
     __syncthreads();
     if (tid == 0) {
-        double total = 0;
-        for (int w = 0; w < kPickThreads / 64; ++w) total += S.near_top[w];
+        double all = 0;
+        for (uint32_t w = 0; w < waves; ++w) all += S.wave_top[w];
         S.exact[k] = 1;
         if (top == NINF) S.state[k] = ROW_NONE;
         else {
             S.infinite[k] = top == -NINF;
-            S.base[k] = (double)A.scores[r] - (log(total) + (top == -NINF ? 0.0 : (double)top));
+            S.base[k] = (double)A.scores[r] - (log(all) + (top == -NINF ? 0.0 : (double)top));
         }
     }
     __threadfence_block();
     __syncthreads();
 }
 
-// Whether candidate a comes before candidate b.
-__device__ __forceinline__ bool before(double sa, uint32_t ra, long long ta, double sb, uint32_t rb, long long tb) {
-    return sa > sb || (sa == sb && (ra < rb || (ra == rb && ta < tb)));
-}
-
-// The best of all threads' candidates, in all threads (row ~0: none).
-__device__ void best_of_all(PickShared& S, double& s, uint32_t& r, long long& t) {
+// The best of all threads' candidates, in all threads (at ~0: none).
+__device__ Candidate best_of_all(PickShared& S, Candidate c) {
     for (int d = 1; d < 64; d *= 2) {
-        const double os = __shfl_xor(s, d);
-        const uint32_t orow = (uint32_t)__shfl_xor((int)r, d);
-        const long long ot = __shfl_xor(t, d);
-        if (orow != ~0u && (r == ~0u || before(os, orow, ot, s, r, t))) { s = os; r = orow; t = ot; }
+        const Candidate o{__shfl_xor(c.score, d), (uint64_t)__shfl_xor((unsigned long long)c.at, d)};
+        if (o.at != ~0ull && (c.at == ~0ull || before(o, c))) c = o;
     }
-    const uint32_t wave = threadIdx.x >> 6;
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) { S.r_score[wave] = s; S.r_row[wave] = r; S.r_at[wave] = t; }
+    if ((threadIdx.x & 63) == 0) S.wave_best[threadIdx.x >> 6] = c;
     __syncthreads();
-    for (int w = 0; w < kPickThreads / 64; ++w)
-        if (S.r_row[w] != ~0u && (r == ~0u || before(S.r_score[w], S.r_row[w], S.r_at[w], s, r, t))) { s = S.r_score[w]; r = S.r_row[w]; t = S.r_at[w]; }
+    for (uint32_t w = 0; w < blockDim.x >> 6; ++w) {
+        const Candidate o = S.wave_best[w];
+        if (o.at != ~0ull && (c.at == ~0ull || before(o, c))) c = o;
+    }
+    return c;
 }
 
-__device__ __forceinline__ void write_choice(const BeamSelect& A, const PickShared& S, uint32_t g, uint32_t n, bool any, double s, uint32_t k, int32_t token) {
+__device__ __forceinline__ void write_choice(const BeamSelect& A, uint32_t g, uint32_t n, bool any, const Candidate& c) {
     const size_t at = (size_t)g * A.n_out + n;
-    A.out_scores[at] = any ? (float)s : NINF;
-    A.out_parents[at] = any ? (int32_t)(g * A.beams + k) : -1;
-    A.out_tokens[at] = any ? token : -1;
-    if (A.out_finished) A.out_finished[at] = !any || token < 0 || token == A.eos_id;
+    const int32_t token = any ? (int32_t)((uint32_t)c.at - 1u) : -1;
+    A.out_scores[at] = any ? (float)c.score : NINF;
+    A.out_parents[at] = any ? (int32_t)(g * A.beams + (uint32_t)(c.at >> 32)) : -1;
+    A.out_tokens[at] = token;
+    if (A.out_finished) A.out_finished[at] = token < 0 || token == A.eos_id;
+}
+
+// Too many are too much alike (logits that are all the same): all sums in 64 bits, then the best block n times, and the best candidate of
+// these blocks n times, each the next one after the one before.
+template <class E>
+__device__ __attribute__((noinline)) void pick_one_by_one(const BeamSelect& A, PickShared& S, uint32_t g) {
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6, K = A.beams, N = A.n_out, n_blocks = A.pieces * kBeamPieceBlocks;
+    const double none = -(double)__builtin_inff();
+    for (uint32_t k = 0; k < K; ++k) if (S.state[k] == ROW_LIVE && !S.exact[k]) repair_row<E>(A, S, g, k);
+    uint32_t n_found = 0;
+    Candidate last{0, ~0ull};
+    for (; n_found < N; ++n_found) {
+        Candidate c{none, ~0ull};
+        for (uint32_t k = wave; k < K; k += waves) {
+            if (S.state[k] != ROW_LIVE) continue;
+            for (uint32_t b = lane; b < n_blocks; b += 64) {
+                const Candidate o{score_of(S, k, A.block_max[(size_t)(g * K + k) * n_blocks + b]), place_of(k, b)};
+                if (o.score > none && (last.at == ~0ull || before(last, o)) && (c.at == ~0ull || before(o, c))) c = o;
+            }
+        }
+        c = best_of_all(S, c);
+        if (c.at == ~0ull) break;
+        if (tid == 0) S.blocks[n_found] = (uint32_t)(c.at >> 32) << kRowShift | ((uint32_t)c.at - 1);
+        last = c;
+    }
+    __syncthreads();
+    last.at = ~0ull;
+    for (uint32_t n = 0; n < N; ++n) {
+        Candidate c{none, ~0ull};
+        for (uint32_t i = wave; i < n_found; i += waves) {
+            const uint32_t k = S.blocks[i] >> kRowShift, b = S.blocks[i] & kRowBits, r = g * K + k;
+            const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
+            const long long t0 = (long long)b * kBeamBlock - before_row(row) + lane;
+            for (int d = 0; d < kBeamBlock; d += 64) {
+                const long long t = t0 + d;
+                if (t < 0 || t >= A.V || !token_allowed(A, r, t)) continue;
+                const Candidate o{score_of(S, k, Elem<E>::load(row + t)), place_of(k, t)};
+                if (o.score > none && (last.at == ~0ull || before(last, o)) && (c.at == ~0ull || before(o, c))) c = o;
+            }
+        }
+        if (tid < K && S.state[tid] == ROW_ENDED) {
+            const Candidate o{S.base[tid], place_of(tid, -1)};
+            if ((last.at == ~0ull || before(last, o)) && (c.at == ~0ull || before(o, c))) c = o;
+        }
+        c = best_of_all(S, c);
+        if (tid == 0) write_choice(A, g, n, c.at != ~0ull, c);
+        if (c.at == ~0ull) c = Candidate{none, ~0ull - 1};           // nothing comes after
+        last = c;
+    }
 }
 
 template <class E>
 __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamSelect A) {
     __shared__ PickShared S;
-    const uint32_t g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), K = A.beams, n_blocks = A.pieces * kBeamPieceBlocks, N = A.n_out;
-    constexpr uint32_t WAVES = kPickThreads / 64;
-    for (uint32_t i = tid; i < kPickBins; i += kPickThreads) S.bins[i] = 0;
-    if (tid == 0) S.n_blocks = S.n_elems = S.any = S.found = 0;
-    __syncthreads();
-    // the rows' sums
-    double top = -(double)__builtin_inff();                          // no score is above it
-    for (uint32_t k = wave; k < K; k += WAVES) {
-        const uint32_t r = g * K + k;
-        const float s = A.scores[r];
-        uint32_t state = !(s > NINF && s < -NINF) ? ROW_NONE : A.finished && A.finished[r] != 0 ? ROW_ENDED : ROW_LIVE, repair = 0;
-        double base = s;
-        if (state == ROW_LIVE) {
-            const float2* const stats = A.stats + (size_t)r * A.pieces;
-            float m = NINF;
-            bool odd = false;
-            for (uint32_t p = lane; p < A.pieces; p += 64) {
-                const float2 v = stats[p];
-                odd |= !(v.y < -NINF) || v.x != v.x || (v.x > NINF && !(v.x > -1e38f && v.x < 1e38f));
-                m = v.x > m ? v.x : m;
-            }
-            for (int d = 1; d < 64; d *= 2) { const float o = __shfl_xor(m, d); m = o > m ? o : m; }
-            // a NaN or an infinity among what counts, or magnitudes that the sum's exponents cannot take: from the logits again
-            repair = __ballot(odd) != 0;
-            if (repair) {}
-            else if (m == NINF) state = ROW_NONE;
-            else {
-                // a piece's sum is of 2^(x * LOG2E - c), c = the rounded product of its maximum and LOG2E; LOG2E itself is off by `off`
-                const double off = (double)LOG2E - 1.4426950408889634073599, mc = (double)__fmul_rn(m, LOG2E) - (double)m * off;
-                double sum = 0;
-                for (uint32_t p = lane; p < A.pieces; p += 64) {
-                    const float2 v = stats[p];
-                    if (v.x > NINF) sum += (double)v.y * exp2((double)__fmul_rn(v.x, LOG2E) - (double)v.x * off - mc);
-                }
-                for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-                base -= log(sum) + mc * LN2;
-                top = base + m > top ? base + m : top;
-            }
-        } else if (state == ROW_ENDED) top = base > top ? base : top;
-        if (lane == 0) {
-            S.state[k] = state; S.base[k] = base; S.infinite[k] = 0; S.exact[k] = state != ROW_LIVE; S.repair[k] = repair;
-            if (repair) S.any = 1;
-        }
+    const uint32_t g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x >> 6, K = A.beams, N = A.n_out, pieces = A.pieces;
+    constexpr double none = -(double)__builtin_inff();
+    // 16 lanes of a row: the row's sum
+    const uint32_t k = tid >> 4, part = tid & 15, r = g * K + k;
+    const Global<const Vec4> stats = (Global<const Vec4>)(A.stats + (size_t)r * pieces);
+    const bool mine = k < K;
+    float s = NINF, best[kPickHeld];
+    Vec4 held[kPickHeld];
+    bool ended = false;
+    if (mine) {
+        _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) held[i] = stats[min(part + i * 16, pieces - 1)];
+        s = ((Global<const float>)A.scores)[r];
+        if (A.finished) ended = ((Global<const int32_t>)A.finished)[r] != 0;
     }
-    if (lane == 0) S.near_top[wave] = top;
-    __syncthreads();
-    for (uint32_t w = 0; w < WAVES; ++w) top = S.near_top[w] > top ? S.near_top[w] : top;
-    if (S.any) {                                                     // (the same in all threads)
-        for (uint32_t k = 0; k < K; ++k) {
-            if (!S.repair[k]) continue;
-            repair_row<E>(A, S, g, k);
-            // (a bound: no logit of the row is above its largest)
-            if (S.state[k] != ROW_LIVE) continue;
-            float m = NINF;
-            for (uint32_t b = lane; b < n_blocks; b += 64) { const float o = A.block_max[(size_t)(g * K + k) * n_blocks + b]; m = o > m ? o : m; }
-            for (int d = 1; d < 64; d *= 2) { const float o = __shfl_xor(m, d); m = o > m ? o : m; }
-            const double s = score_of(S, k, m);
-            top = s > top ? s : top;
+    for (uint32_t i = tid; i < kPickBins; i += blockDim.x) S.bins[i] = 0;
+    if (tid == 0) S.n_pieces = S.n_blocks = S.n_elems = 0;
+    uint32_t state = !(s > NINF && s < -NINF) ? ROW_NONE : ended ? ROW_ENDED : ROW_LIVE, repair = 0;
+    double base = s, top = none;                                     // top: no score is above it
+    if (state == ROW_LIVE) {
+        float m = NINF;
+        bool odd = false;
+        auto look = [&](const Vec4& v) {
+            const float x = __uint_as_float(v[0]), y = __uint_as_float(v[1]);
+            odd |= x != x || y != y;
+            m = x > m ? x : m;
+        };
+        _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) {
+            if (part + i * 16 >= pieces) held[i] = stats_of(NINF, 0.f, NINF);
+            look(held[i]);
+            best[i] = __uint_as_float(held[i][2]);
         }
+        for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) look(stats[p]);
+        m = largest_of_16(m);
+        // a NaN or an infinity among what counts, or magnitudes that the sum's exponents cannot take: from the logits again
+        odd |= !(m < 1e6f) || (m > NINF && m < -1e6f);
+        repair = ((__ballot(odd) >> (lane & 48)) & 0xFFFF) != 0;
+        // A piece's sum is of 2^(x * LOG2E - c), c = the rounded product of its maximum and LOG2E; LOG2E itself is off by `off`.
+        const double off = (double)LOG2E - 1.4426950408889634073599, mc = (double)__fmul_rn(m, LOG2E) - (double)m * off;
+        double sum = 0;
+        auto add = [&](const Vec4& v) {
+            const float x = __uint_as_float(v[0]);
+            const double t = (double)__fmul_rn(x, LOG2E) - (double)x * off - mc;
+            if (t > -200) sum += (double)__uint_as_float(v[1]) * exp2_of(t);
+        };
+        _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) if (i * 16u < pieces) add(held[i]);     // (the same in all lanes)
+        for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) add(stats[p]);
+        sum = sum_of_16(sum);
+        if (m == NINF) { if (!repair) state = ROW_NONE; }
+        else {
+            base -= log_of(sum) + mc * LN2;
+            top = base + m;
+        }
+    } else if (state == ROW_ENDED) top = base;
+    if (mine && part == 0) { S.state[k] = state; S.base[k] = base; S.infinite[k] = 0; S.exact[k] = state != ROW_LIVE; S.repair[k] = repair; }
+    {
+        const double a = __shfl_xor(top, 16), ab = top > a ? top : a, c = __shfl_xor(ab, 32);
+        top = ab > c ? ab : c;
+    }
+    if (lane == 0) S.wave_top[wave] = top;
+    if (__syncthreads_or((int)repair)) {
+        for (uint32_t q = 0; q < K; ++q) if (S.repair[q]) repair_row<E>(A, S, g, q);
+        top = none;
+        if (mine) {
+            state = S.state[k];
+            float m = NINF;
+            if (state == ROW_LIVE) {
+                _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) { best[i] = part + i * 16 < pieces ? ((Global<const float>)(stats + part + i * 16))[2] : NINF; m = best[i] > m ? best[i] : m; }
+                for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) { const float o = ((Global<const float>)(stats + p))[2]; m = o > m ? o : m; }
+                top = m > NINF ? score_of(S, k, m) : none;           // (no logit of a row is above its largest)
+            } else if (state == ROW_ENDED) top = S.base[k];
+        }
+        for (int d = 1; d < 64; d *= 2) { const double o = __shfl_xor(top, d); top = o > top ? o : top; }
+        if (lane == 0) S.wave_top[wave] = top;
         __syncthreads();
     }
-    const uint32_t steps = (n_blocks + 63) / 64, units = K * steps;
-    // how many blocks (and ended beams) have their best score in each bin
-    for (uint32_t u = wave; u < units; u += WAVES) {
-        const uint32_t k = u / steps, b = u % steps * 64 + lane;
-        if (S.state[k] != ROW_LIVE || b >= n_blocks) continue;
-        const double s = score_of(S, k, A.block_max[(size_t)(g * K + k) * n_blocks + b]);
-        if (s > -(double)__builtin_inff()) atomicAdd(&S.bins[bin_of(top, s)], 1u);
-    }
-    if (tid < K && S.state[tid] == ROW_ENDED) atomicAdd(&S.bins[bin_of(top, S.base[tid])], 1u);
+    for (uint32_t w = 0; w < waves; ++w) top = S.wave_top[w] > top ? S.wave_top[w] : top;
+    // how many pieces (and ended beams) have their best score in each bin
+    uint32_t bin[kPickHeld];
+    auto bin_if = [&](uint32_t row, float m) {
+        const double v = score_of(S, row, m);
+        return m > NINF && v > none ? bin_of(top, v) : (uint32_t)kPickBins;
+    };
+    auto count = [&](uint32_t b) { if (b < kPickBins) atomicAdd(&S.bins[bin_at(b)], 1u); };
+    if (state == ROW_LIVE) {
+        _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) { bin[i] = bin_if(k, best[i]); count(bin[i]); }
+        for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) count(bin_if(k, ((Global<const float>)(stats + p))[2]));
+    } else if (state == ROW_ENDED && part == 0) count(bin_of(top, S.base[k]));
     __syncthreads();
-    if (wave == 0) {
-        constexpr uint32_t EACH = kPickBins / 64;
-        uint32_t mine = 0;
-        for (uint32_t i = 0; i < EACH; ++i) mine += S.bins[lane * EACH + i];
-        uint32_t upto = mine;
-        for (int d = 1; d < 64; d *= 2) { const uint32_t o = (uint32_t)__shfl_up((int)upto, d); if ((int)lane >= d) upto += o; }
-        const unsigned long long reached = __ballot(upto >= N);
-        if (reached == 0) { if (lane == 0) S.last_bin = kPickBins - 1; }
-        else if ((int)lane == __ffsll((long long)reached) - 1) {
-            uint32_t n = upto - mine, i = 0;
-            for (; i < EACH; ++i) { n += S.bins[lane * EACH + i]; if (n >= N) break; }
-            S.last_bin = lane * EACH + i + 1;                        // one bin more: what lies within A.near of the n-th best
-        }
-    }
-    __syncthreads();
-    const uint32_t last_bin = S.last_bin;
-    // the blocks that can hold one of the n best, and of them and the ended beams the candidates that can be one
-    for (uint32_t u = wave; u < units; u += WAVES) {
-        const uint32_t k = u / steps, b = u % steps * 64 + lane;
-        if (S.state[k] != ROW_LIVE || b >= n_blocks) continue;
-        const double s = score_of(S, k, A.block_max[(size_t)(g * K + k) * n_blocks + b]);
-        if (s > -(double)__builtin_inff() && bin_of(top, s) <= last_bin) {
-            const uint32_t i = atomicAdd(&S.n_blocks, 1u);
-            if (i < kPickBlocks) S.blocks[i] = k * n_blocks + b;
-        }
-    }
-    if (tid < K && S.state[tid] == ROW_ENDED) {
-        const uint32_t i = atomicAdd(&S.n_elems, 1u);
-        S.score[i] = S.base[tid]; S.x[i] = 0.f; S.token[i] = -1; S.row[i] = (uint16_t)tid;
-    }
-    __syncthreads();
-    const uint32_t listed = S.n_blocks < kPickBlocks ? S.n_blocks : kPickBlocks;
-    for (uint32_t i = wave; i < listed; i += WAVES) {
-        const uint32_t k = S.blocks[i] / n_blocks, b = S.blocks[i] % n_blocks, r = g * K + k;
-        const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
-        const long long t0 = (long long)b * kBeamBlock - before_row(row) + lane;
-        for (int c = 0; c < kBeamBlock; c += 64) {
-            const long long t = t0 + c;
-            if (t < 0 || t >= A.V || !token_allowed(A, r, t)) continue;
-            const float x = Elem<E>::value(row[t]);
-            const double s = score_of(S, k, x);
-            if (!(s > -(double)__builtin_inff()) || bin_of(top, s) > last_bin) continue;
-            const uint32_t at = atomicAdd(&S.n_elems, 1u);
-            if (at < kPickElems) { S.score[at] = s; S.x[at] = x; S.token[at] = (int32_t)t; S.row[at] = (uint16_t)k; }
-        }
-    }
-    __syncthreads();
-    if (S.n_blocks <= kPickBlocks && S.n_elems <= kPickElems) {
-        const uint32_t R = S.n_elems;
-        for (;;) {
-            // a candidate's place is the number of candidates before it
-            for (uint32_t i = tid; i < R; i += kPickThreads) {
-                const double s = S.score[i];
-                const uint32_t k = S.row[i];
-                const int32_t t = S.token[i];
-                uint32_t place = 0;
-                for (uint32_t j = 0; j < R; ++j) place += before(S.score[j], S.row[j], S.token[j], s, k, t) ? 1u : 0u;
-                S.sorted[place] = (uint16_t)i;
-            }
-            if (tid < K) S.repair[tid] = 0;
-            if (tid == 0) S.any = 0;
-            __syncthreads();
-            // Neighbours of different rows that are too close for their sums, among the chosen and those that are as close to the last
-            // of them: these rows' sums in 64 bits.  (Two that are close and not neighbours have neighbours of different rows between them.)
-            for (uint32_t n = tid; n + 1 < R; n += kPickThreads) {
-                const uint32_t i = S.sorted[n], j = S.sorted[n + 1], ki = S.row[i], kj = S.row[j];
-                if (ki == kj || (S.exact[ki] && S.exact[kj]) || S.score[i] - S.score[j] > A.near) continue;
-                if (n + 1 <= N || !(S.score[S.sorted[N - 1]] - S.score[j] > A.near)) { S.repair[ki] = S.repair[kj] = 1; S.any = 1; }
-            }
-            __syncthreads();
-            if (!S.any) break;
-            for (uint32_t k = 0; k < K; ++k) if (S.repair[k] && !S.exact[k]) repair_row<E>(A, S, g, k);
-            __syncthreads();
-            for (uint32_t i = tid; i < R; i += kPickThreads) if (S.token[i] >= 0) S.score[i] = score_of(S, S.row[i], S.x[i]);
-            __syncthreads();
-        }
-        if (tid < N) {
-            const bool any = tid < R;
-            const uint32_t i = any ? S.sorted[tid] : 0;
-            write_choice(A, S, g, tid, any, any ? S.score[i] : 0, any ? S.row[i] : 0, any ? S.token[i] : -1);
-        }
-        return;
-    }
-    // Too many are too much alike (logits that are all the same): all sums in 64 bits, then the best block n times, and the best
-    // candidate of these blocks n times, each the next one after the one before.
-    for (uint32_t k = 0; k < K; ++k) if (S.state[k] == ROW_LIVE && !S.exact[k]) repair_row<E>(A, S, g, k);
-    const double none = -(double)__builtin_inff();
-    uint32_t n_found = 0;
+    uint32_t last_bin = kPickBins - 1;                               // (every wavefront for itself)
     {
-        double ls = 0;
-        uint32_t lr = ~0u;
-        long long lb = 0;
-        while (n_found < N) {
-            double s = none;
-            uint32_t k1 = ~0u;
-            long long b1 = 0;
-            for (uint32_t u = wave; u < units; u += WAVES) {
-                const uint32_t k = u / steps, b = u % steps * 64 + lane;
-                if (S.state[k] != ROW_LIVE || b >= n_blocks) continue;
-                const double v = score_of(S, k, A.block_max[(size_t)(g * K + k) * n_blocks + b]);
-                if (!(v > none) || (lr != ~0u && !before(ls, lr, lb, v, k, b))) continue;
-                if (k1 == ~0u || before(v, k, b, s, k1, b1)) { s = v; k1 = k; b1 = b; }
-            }
-            best_of_all(S, s, k1, b1);
-            if (k1 == ~0u) break;
-            if (tid == 0) S.blocks[n_found] = k1 * n_blocks + (uint32_t)b1;
-            ++n_found;
-            ls = s; lr = k1; lb = b1;
+        uint32_t n[16], sum = 0;
+        _Pragma("unroll") for (uint32_t i = 0; i < 16; ++i) { n[i] = S.bins[i * 64 + lane]; sum += n[i]; }
+        const uint32_t upto = count_upto(sum);
+        const unsigned long long reached = __ballot(upto >= N);
+        if (reached != 0) {
+            uint32_t at = upto - sum, b = 0;
+            _Pragma("unroll") for (uint32_t i = 0; i < 16; ++i) { at += n[i]; b += at < N ? 1u : 0u; }
+            // one bin more: what lies within A.near of the n-th best
+            last_bin = (uint32_t)__builtin_amdgcn_readlane((int)(lane * 16 + b + 1), __ffsll((long long)reached) - 1);
+        }
+    }
+    // the pieces that can hold one of the n best, of them the blocks, of them and the ended beams the candidates that can be one
+    auto list_piece = [&](uint32_t p) { const uint32_t at = atomicAdd(&S.n_pieces, 1u); if (at < kPickListed) S.pieces[at] = k << kRowShift | p; };
+    auto list_candidate = [&](double v, uint64_t at, float x) {
+        const uint32_t i = atomicAdd(&S.n_elems, 1u);
+        if (i < kPickElems) { S.found[i] = Candidate{v, at}; S.x[i] = x; }
+    };
+    if (state == ROW_LIVE) {
+        _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) if (bin[i] <= last_bin) list_piece(part + i * 16);
+        for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) if (bin_if(k, ((Global<const float>)(stats + p))[2]) <= last_bin) list_piece(p);
+    } else if (state == ROW_ENDED && part == 0) list_candidate(S.base[k], place_of(k, -1), 0.f);
+    __syncthreads();
+    const uint32_t n_pieces = min(S.n_pieces, (uint32_t)kPickListed);
+    for (uint32_t i = tid; i < n_pieces * kBeamPieceBlocks; i += blockDim.x) {
+        const uint32_t piece = S.pieces[i / kBeamPieceBlocks], row_k = piece >> kRowShift, block = (piece & kRowBits) * kBeamPieceBlocks + i % kBeamPieceBlocks;
+        if (bin_if(row_k, ((Global<const float>)A.block_max)[(size_t)(g * K + row_k) * pieces * kBeamPieceBlocks + block]) > last_bin) continue;
+        const uint32_t at = atomicAdd(&S.n_blocks, 1u);
+        if (at < kPickListed) S.blocks[at] = row_k << kRowShift | block;
+    }
+    for (uint32_t i = tid; i < kPickElems; i += blockDim.x) S.place[i] = 0;
+    __syncthreads();
+    // 16 lanes have a block, each of them 16 tokens
+    const uint32_t listed = min(S.n_blocks, (uint32_t)kPickListed);
+    const double reach = last_bin < kPickBins - 1 ? top - reach_of(last_bin) : none;
+    for (uint32_t i = tid >> 4; i < listed; i += blockDim.x >> 4) {
+        constexpr int EPV = Elem<E>::EPV, VECS = 16 / EPV;
+        const uint32_t block = S.blocks[i], row_k = block >> kRowShift, row_r = g * K + row_k;
+        const E* const row = static_cast<const E*>(A.logits) + (long long)row_r * A.row_stride;
+        const int t0 = (int)((block & kRowBits) * kBeamBlock + 16 * part) - before_row(row);
+        const bool inner = t0 >= 0 && t0 + 16 <= A.V;
+        Vec4 raw[VECS];
+        uint32_t ok = 0xFFFF;
+        if (A.bitmask) {
+            const Global<const uint32_t> bm = (Global<const uint32_t>)(A.bitmask + (long long)row_r * A.bm_stride);
+            const uint64_t both = (uint64_t)bm[min(max(t0 + 15, 0), A.V - 1) >> 5] << 32 | bm[min(max(t0, 0), A.V - 1) >> 5];
+            const bool next = (max(t0, 0) & 31) + 16 > 32;           // (of a word that is its own neighbour the lower half is read)
+            ok = t0 >= 0 ? (uint32_t)((next ? both : both & 0xFFFFFFFFu) >> (t0 & 31)) : (uint32_t)both << min(-t0, 16);
+        }
+        if (inner) { _Pragma("unroll") for (int v = 0; v < VECS; ++v) raw[v] = ((Global<const Vec4>)(row + t0))[v]; }
+        else {
+            _Pragma("unroll") for (int v = 0; v < VECS; ++v) raw[v] = Elem<E>::gather(row, t0 + v * EPV, A.V);
+            if (t0 < 0) ok &= 0xFFFFu << min(-t0, 16);
+            if (t0 + 16 > A.V) ok &= t0 < A.V ? 0xFFFFu >> (t0 + 16 - A.V) : 0u;
+        }
+        float x[16];
+        _Pragma("unroll") for (int v = 0; v < VECS; ++v) Elem<E>::unpack(raw[v], x + v * EPV);
+        // a bound in 32 bits first
+        const double least = reach - S.base[row_k];
+        const float bound = (float)least - (__builtin_fabsf((float)least) * 1e-6f + 1e-3f);
+        uint32_t hits = 0;
+        _Pragma("unroll") for (int c = 0; c < 16; ++c) hits |= x[c] >= bound ? 1u << c : 0u;
+        for (hits &= ok; hits != 0; hits &= hits - 1) {
+            const int c = __ffs((int)hits) - 1;
+            float v = x[0];
+            _Pragma("unroll") for (int q = 1; q < 16; ++q) v = c == q ? x[q] : v;
+            if (!(v > NINF)) continue;
+            const double score = score_of(S, row_k, v);
+            if (score > none && bin_of(top, score) <= last_bin) list_candidate(score, place_of(row_k, t0 + c), v);
         }
     }
     __syncthreads();
-    double ls = 0;
-    uint32_t lr = ~0u;
-    long long lt = 0;
-    for (uint32_t n = 0; n < N; ++n) {
-        double s = none;
-        uint32_t k1 = ~0u;
-        long long t1 = 0;
-        for (uint32_t i = wave; i < n_found; i += WAVES) {
-            const uint32_t k = S.blocks[i] / n_blocks, b = S.blocks[i] % n_blocks, r = g * K + k;
-            const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
-            const long long t0 = (long long)b * kBeamBlock - before_row(row) + lane;
-            for (int c = 0; c < kBeamBlock; c += 64) {
-                const long long t = t0 + c;
-                if (t < 0 || t >= A.V || !token_allowed(A, r, t)) continue;
-                const double v = score_of(S, k, Elem<E>::value(row[t]));
-                if (!(v > none) || (lr != ~0u && !before(ls, lr, lt, v, k, t))) continue;
-                if (k1 == ~0u || before(v, k, t, s, k1, t1)) { s = v; k1 = k; t1 = t; }
+    if (S.n_pieces > kPickListed || S.n_blocks > kPickListed || S.n_elems > kPickElems) { pick_one_by_one<E>(A, S, g); return; }
+    const uint32_t R = S.n_elems;
+    for (;;) {
+        // A candidate's place is the number of candidates before it: a wavefront compares 64 candidates with its part of all.
+        if (R <= 64) {
+            if (wave == 0) {
+                const Candidate c = S.found[lane < R ? lane : 0];
+                uint32_t n = 0;
+                _Pragma("unroll 4") for (uint32_t j = 0; j < R; ++j) n += before(S.found[j], c) ? 1u : 0u;
+                if (lane < R) S.sorted[n] = (uint16_t)lane;
             }
+        } else {
+            const uint32_t chunks = (R + 63) / 64, parts = max(waves / chunks, 1u);
+            for (uint32_t w = wave; w < chunks * parts; w += waves) {
+                const uint32_t i = w % chunks * 64 + lane, p = w / chunks, to = (p + 1) * R / parts;
+                const Candidate c = S.found[i < R ? i : 0];
+                uint32_t n = 0;
+                _Pragma("unroll 4") for (uint32_t j = p * R / parts; j < to; ++j) n += before(S.found[j], c) ? 1u : 0u;
+                if (i < R && n != 0) atomicAdd(&S.place[i], n);
+            }
+            __syncthreads();
+            for (uint32_t i = tid; i < R; i += blockDim.x) { S.sorted[S.place[i]] = (uint16_t)i; S.place[i] = 0; }
         }
-        if (tid < K && S.state[tid] == ROW_ENDED) {
-            const double v = S.base[tid];
-            if ((lr == ~0u || before(ls, lr, lt, v, tid, -1)) && (k1 == ~0u || before(v, tid, -1, s, k1, t1))) { s = v; k1 = tid; t1 = -1; }
+        if (tid < K) S.repair[tid] = 0;
+        __syncthreads();
+        // Neighbours of different rows that are too close for their sums, among the chosen and those that are as close to the last of
+        // them: these rows' sums in 64 bits.  (Two that are close and not neighbours have neighbours of different rows between them.)
+        int any = 0;
+        for (uint32_t n = tid; n + 1 < R; n += blockDim.x) {
+            const Candidate a = S.found[S.sorted[n]], b = S.found[S.sorted[n + 1]];
+            const uint32_t ka = (uint32_t)(a.at >> 32), kb = (uint32_t)(b.at >> 32);
+            if (ka == kb || (S.exact[ka] && S.exact[kb]) || a.score - b.score > A.near) continue;
+            if (n + 1 <= N || !(S.found[S.sorted[N - 1]].score - b.score > A.near)) { S.repair[ka] = S.repair[kb] = 1; any = 1; }
         }
-        best_of_all(S, s, k1, t1);
-        if (tid == 0) write_choice(A, S, g, n, k1 != ~0u, s, k1, (int32_t)t1);
-        if (k1 != ~0u) { ls = s; lr = k1; lt = t1; }
-        else { lr = K; ls = none; }                                  // nothing comes after
+        if (!__syncthreads_or(any)) break;
+        for (uint32_t q = 0; q < K; ++q) if (S.repair[q] && !S.exact[q]) repair_row<E>(A, S, g, q);
+        for (uint32_t i = tid; i < R; i += blockDim.x)
+            if ((uint32_t)S.found[i].at != 0) S.found[i].score = score_of(S, (uint32_t)(S.found[i].at >> 32), S.x[i]);
+        __syncthreads();
     }
+    if (tid < N) write_choice(A, g, tid, tid < R, tid < R ? S.found[S.sorted[tid]] : Candidate{0, 0});
 }
 
 // ---- matcher slots --------------------------------------------------------------------------------------------------
@@ -594,17 +780,19 @@ template <class E>
 static void launch_beam_select_as(const BeamSelect& A, hipStream_t stream) {
     const uint32_t rows = A.groups * A.beams;
     auto* const kernel = !A.bitmask ? k_beam_scan<E, 0> : A.over_all ? k_beam_scan<E, 2> : k_beam_scan<E, 1>;
+    const uint32_t waves = (uint64_t)A.pieces * rows <= 512 ? 1 : kScanWaves;
     for (uint32_t first = 0; first < rows; first += 65535) {         // grid.y limit
         const uint32_t n = std::min<uint32_t>(65535, rows - first);
-        hipLaunchKernelGGL(kernel, dim3((A.pieces + kScanWaves - 1) / kScanWaves, n), dim3(64 * kScanWaves), 0, stream, A, first);
+        hipLaunchKernelGGL(kernel, dim3((A.pieces + waves - 1) / waves, n), dim3(64 * waves), 0, stream, A, first);
     }
-    hipLaunchKernelGGL(k_beam_pick<E>, dim3(A.groups), dim3(kPickThreads), 0, stream, A);
+    const uint32_t threads = std::min<uint32_t>(kPickThreads, std::max<uint32_t>(256, (16 * std::max(A.beams, A.n_out + A.n_out / 2) + 63) / 64 * 64));
+    hipLaunchKernelGGL(k_beam_pick<E>, dim3(A.groups), dim3(threads), 0, stream, A);
 }
 
 void launch_beam_select(const BeamSelect& A, hipStream_t stream) {
     if (A.groups == 0) return;
     if (A.dtype == XG2_F32) launch_beam_select_as<float>(A, stream);
-    else launch_beam_select_as<Bf16>(A, stream);
+    else launch_beam_select_as<uint16_t>(A, stream);
 }
 
 void launch_batch_reorder(const BatchDev& D, uint32_t beams, const int32_t* parents_dev, int32_t* status_dev, hipStream_t stream) {

@@ -22,7 +22,8 @@ struct BeamSelect {
     const void* logits; long long row_stride;               // elements
     const uint32_t* bitmask; long long bm_stride;           // null: everything is allowed
     const float* scores; const int32_t* finished;           // [rows]; finished may be null
-    float2* stats;                                          // [rows * pieces] of what counts in the softmax: maximum and sum of exponentials relative to it
+    float4* stats;                                          // [rows * pieces]: of what counts in the softmax the maximum and the sum of exponentials relative
+                                                            // to it, and the largest allowed logit
     float* block_max;                                       // [rows * pieces * kBeamPieceBlocks] largest allowed logit
     float* out_scores; int32_t* out_parents; int32_t* out_tokens; int32_t* out_finished;
     uint32_t groups, beams, n_out, pieces;
