@@ -5,6 +5,7 @@
 //   k_beam_reorder_rows  the same for rows of a caller's buffer, in place
 //   k_beam_backtrace     sequences from the steps' tokens and parents
 #include <algorithm>
+#include <cstddef>
 
 #include "beam.hpp"
 
@@ -662,47 +663,62 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamSelect A) {
 // ---- matcher slots --------------------------------------------------------------------------------------------------
 // One workgroup per group of beams, a wavefront for up to SLOTS of its slots.  A slot's context has two buffers, and nobody reads the one
 // that is not its own state, so the parent's goes there at once; the slot's record and its frontier planes have one place, so these
-// wait in registers until all wavefronts of the group have read theirs.
+// wait in registers (the record a word a lane) until all wavefronts of the group have read theirs.  Bound by latency: three loads in a row
+// (parents, records, context), so the first 64 of everything in a context are asked for together, without waiting for the counts (a slot
+// has room for that many and more), like the planes.
+constexpr uint32_t kRowWords = sizeof(FillRow) / 4;
+static_assert(kRowWords <= 64 && offsetof(FillRow, front_off) == 0 && offsetof(FillRow, front_n) == 4 && offsetof(FillRow, item_off) == 8 && offsetof(FillRow, item_n) == 12 &&
+              offsetof(FillRow, wait_base) == 16 && offsetof(FillRow, waitoff_off) == 20 && offsetof(FillRow, H) == 24 && offsetof(FillRow, pad) == 36 && offsetof(FillRow, n_wait) == 44,
+              "k_batch_reorder has a record a word a lane");
 template <int SLOTS>
-__global__ __launch_bounds__(1024) void k_batch_reorder(BatchDev D, uint32_t K, const int32_t* parents, int32_t* status) {
+__global__ __launch_bounds__(1024) void k_batch_reorder(const int32_t* parents, FillRow* rows, uint32_t K, BatchDev D, int32_t* status) {
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), waves = blockDim.x >> 6, first = blockIdx.x * K;
     uint64_t plane[SLOTS];
-    FillRow row[SLOTS];
-    bool moved[SLOTS];
+    uint32_t word[SLOTS];
+    bool moves[SLOTS];
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
         const uint32_t k = wave + (uint32_t)j * waves, b = first + k;
-        moved[j] = false;
+        moves[j] = false;
         if (k >= K) continue;
-        const int32_t p = parents[b];
+        const int32_t p = (int32_t)uniform((uint32_t)((Global<const int32_t>)parents)[b]);
         const bool in_group = p >= 0 && (uint32_t)p >= first && (uint32_t)p < first + K;
-        if (status && lane == 0) status[b] = in_group || p == -1 ? kAccOk : kAccInvalid;
+        if (status && lane == 0) ((Global<int32_t>)status)[b] = in_group || p == -1 ? kAccOk : kAccInvalid;
         if (!in_group || (uint32_t)p == b) continue;
-        const uint32_t to = D.rows[b].pad[0] ^ 1u;
+        moves[j] = true;
+        const uint32_t own = ((Global<const uint32_t>)(rows + b))[offsetof(FillRow, pad) / 4], w = lane < kRowWords ? ((Global<const uint32_t>)(rows + p))[lane] : 0u;
+        auto field = [&](uint32_t at) { return (uint32_t)__builtin_amdgcn_readlane((int)w, (int)at); };
+        const uint32_t to = uniform(own) ^ 1u, item_n = field(3), H = field(6), n_wait = field(11);
+        const Global<const uint32_t> items = (Global<const uint32_t>)(D.items + field(2)), off = (Global<const uint32_t>)(D.wait_off + field(5));
+        const Global<const uint64_t> wait = (Global<const uint64_t>)(D.wait + field(4));
         const size_t slot = (size_t)to * D.B + b;
-        FillRow r = D.rows[p];
-        plane[j] = lane < r.front_n ? D.front[(size_t)r.front_off + lane] : 0;
-        const uint32_t* const items = D.items + r.item_off;
-        const uint32_t* const off = D.wait_off + r.waitoff_off;
-        const uint2* const wait = D.wait + r.wait_base;
-        for (uint32_t i = lane; i < r.item_n; i += 64) D.items[slot * D.KI + i] = items[i];
-        for (uint32_t i = lane; i <= r.H; i += 64) D.wait_off[slot * (D.KH + 1) + i] = off[i];
-        for (uint32_t i = lane; i < r.n_wait; i += 64) D.wait[slot * D.KW + i] = wait[i];
-        r.front_off = b * D.KF;
-        r.item_off = (uint32_t)(slot * D.KI); r.wait_base = (uint32_t)(slot * D.KW); r.waitoff_off = (uint32_t)(slot * (D.KH + 1));
-        r.pad[0] = to;
-        row[j] = r;
-        moved[j] = true;
+        const Global<uint32_t> items_out = (Global<uint32_t>)(D.items + slot * D.KI), off_out = (Global<uint32_t>)(D.wait_off + slot * (D.KH + 1));
+        const Global<uint64_t> wait_out = (Global<uint64_t>)(D.wait + slot * D.KW);
+        const uint32_t item0 = items[lane], off0 = off[lane];
+        const uint64_t wait0 = wait[lane];
+        plane[j] = lane < D.KF ? ((Global<const uint64_t>)D.front)[(size_t)field(0) + lane] : 0u;
+        if (lane < item_n) items_out[lane] = item0;
+        if (lane <= H) off_out[lane] = off0;
+        if (lane < n_wait) wait_out[lane] = wait0;
+        for (uint32_t i = lane + 64; i <= H; i += 64) off_out[i] = off[i];
+        for (uint32_t i = lane + 64; i < n_wait; i += 64) wait_out[i] = wait[i];
+        // the record as it will be: places of its own, the rest the parent's
+        word[j] = w;
+        if (lane == 0) word[j] = b * D.KF;
+        if (lane == 2) word[j] = (uint32_t)(slot * D.KI);
+        if (lane == 4) word[j] = (uint32_t)(slot * D.KW);
+        if (lane == 5) word[j] = (uint32_t)(slot * (D.KH + 1));
+        if (lane == offsetof(FillRow, pad) / 4) word[j] = to;
     }
     // (what was loaded is there before any wavefront stores)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
-        if (!moved[j]) continue;
-        const uint32_t b = first + wave + (uint32_t)j * waves;
-        if (lane < row[j].front_n) D.front[(size_t)b * D.KF + lane] = plane[j];
-        if (lane == 0) D.rows[b] = row[j];
+        if (!moves[j]) continue;
+        const uint32_t b = first + wave + (uint32_t)j * waves, n = (uint32_t)__builtin_amdgcn_readlane((int)word[j], 1);
+        if (lane < n) ((Global<uint64_t>)D.front)[(size_t)b * D.KF + lane] = plane[j];
+        if (lane < kRowWords) ((Global<uint32_t>)(rows + b))[lane] = word[j];
     }
 }
 
@@ -753,25 +769,90 @@ __global__ __launch_bounds__(256) void k_beam_reorder_rows(BeamRows A, uint32_t 
 }
 
 // ---- sequences ------------------------------------------------------------------------------------------------------
-// One thread per sequence, from the last step to the first.
-__global__ __launch_bounds__(64) void k_beam_backtrace(BeamTrace A) {
-    const uint32_t g = blockIdx.x, k = threadIdx.x;
-    if (k >= A.beams) return;
-    const uint32_t first = g * A.beams;
-    int32_t* const out = A.out + (int64_t)(first + k) * A.out_stride;
-    int32_t length = 0;
-    int64_t row = first + k;
-    for (int64_t t = (int64_t)A.steps - 1; t >= 0; --t) {
-        int32_t token = -1;
-        if (row >= 0) {
-            token = A.tokens[t * A.step_stride + row];
-            row = A.parents[t * A.step_stride + row];
-            if (row < (int64_t)first || row >= (int64_t)first + A.beams) row = -1;
+// A chain of as many look-ups as there are steps, one behind the other; but where the beams behind a segment of the steps come from
+// before it does not hang on the other segments.  So the steps are cut into segments, each worked out by WIDTH lanes of a wavefront (a
+// beam each): first every segment's map from the beams behind it to those before it, then the maps of all segments from each one on,
+// put together two and two (in as many rounds as the number of segments has binary digits), then every segment again from the beams
+// that the sequences enter it with, writing their tokens.  A step's parents are one load for all beams of a group, which waits for nothing;
+// which of them a beam's is comes from the lane that holds it.  Segments of up to kTraceHeld steps are loaded once and kept in registers.
+constexpr int kTraceThreads = 1024, kTraceHeld = 16;
+template <int WIDTH>
+__global__ __launch_bounds__(kTraceThreads) void k_beam_backtrace(BeamTrace A, uint32_t segments, uint32_t length) {
+    constexpr uint32_t NONE = 255;
+    __shared__ uint8_t maps[2][kTraceThreads];                       // [segment * WIDTH + beam behind it]: the beam before it
+    __shared__ int32_t last[WIDTH];                                  // steps up to and with a sequence's last token
+    const uint32_t g = blockIdx.x, K = A.beams, lane = threadIdx.x & 63, k = lane % WIDTH, base = lane - k, first = g * K, s = threadIdx.x / WIDTH;
+    const uint32_t from = s * length, to = s < segments ? min(from + length, A.steps) : from;
+    const bool mine = k < K;
+    const uint32_t row = first + (mine ? k : 0);
+    const Global<const int32_t> parents = (Global<const int32_t>)A.parents, tokens = (Global<const int32_t>)A.tokens;
+    uint32_t beam[kTraceHeld];                                       // of the parent, NONE if it is not of the group
+    int32_t token[kTraceHeld];
+    // steps from the segment's end on, `done` of them already walked (the loops are the same in all lanes of a wavefront)
+    auto load = [&](uint32_t done, bool with_tokens) {
+        _Pragma("unroll") for (int i = 0; i < kTraceHeld; ++i) {
+            if (from + done + i < to) {
+                const int64_t t = (int64_t)(to - 1 - done - i) * A.step_stride + row;
+                beam[i] = (uint32_t)parents[t] - first;
+                if (with_tokens) token[i] = tokens[t];
+            }
         }
-        out[t] = token;
-        if (token >= 0 && length == 0) length = (int32_t)t + 1;
+    };
+    auto step = [&](uint32_t at, uint32_t next) { return at >= K ? NONE : next < K ? next : NONE; };
+    const bool held = length <= kTraceHeld;
+    load(0, held);
+    if (threadIdx.x < WIDTH) last[threadIdx.x] = 0;
+    uint32_t at = mine ? k : NONE;
+    for (uint32_t done = 0; done < length; done += kTraceHeld) {
+        if (done != 0) load(done, false);
+        _Pragma("unroll") for (int i = 0; i < kTraceHeld; ++i) {
+            const uint32_t next = (uint32_t)__shfl((int)beam[i], (int)(base + at % WIDTH));
+            if (from + done + i < to) at = step(at, next);
+        }
     }
-    if (A.lengths) A.lengths[first + k] = length;
+    maps[0][threadIdx.x] = (uint8_t)at;
+    __syncthreads();
+    // maps[s] becomes the map from the end of all steps to before segment s
+    uint32_t turn = 0;
+    for (uint32_t d = 1; d < segments; d *= 2) {
+        if (s + d < segments) {
+            const uint32_t behind = maps[turn][threadIdx.x + d * WIDTH];
+            at = behind < K ? maps[turn][s * WIDTH + behind] : NONE;
+        }
+        turn ^= 1;
+        maps[turn][threadIdx.x] = (uint8_t)at;
+        __syncthreads();
+    }
+    at = !mine ? NONE : s + 1 < segments ? maps[turn][threadIdx.x + WIDTH] : k;
+    int32_t end = 0;
+    const Global<int32_t> out = (Global<int32_t>)(A.out + (int64_t)row * A.out_stride);
+    for (uint32_t done = 0; done < length; done += kTraceHeld) {
+        if (!held) load(done, true);
+        _Pragma("unroll") for (int i = 0; i < kTraceHeld; ++i) {
+            const int source = (int)(base + at % WIDTH);
+            const uint32_t next = (uint32_t)__shfl((int)beam[i], source);
+            const int32_t t = __shfl(token[i], source);
+            token[i] = at < K ? t : -1;
+            if (from + done + i < to) at = step(at, next);
+        }
+        if (!mine) continue;
+        _Pragma("unroll") for (int i = 0; i < kTraceHeld; i += 4) {
+            const uint32_t n = done + i;
+            if (from + n + 3 < to) {
+                *(Global<Wide4>)(out + (to - 4 - n)) = Wide4{(uint32_t)token[i + 3], (uint32_t)token[i + 2], (uint32_t)token[i + 1], (uint32_t)token[i]};
+                _Pragma("unroll") for (int j = 0; j < 4; ++j) if (token[i + j] >= 0) end = max(end, (int32_t)(to - n - j));
+            } else {
+                _Pragma("unroll") for (int j = 0; j < 4; ++j) {
+                    if (from + n + j >= to) continue;
+                    out[to - 1 - n - j] = token[i + j];
+                    if (token[i + j] >= 0) end = max(end, (int32_t)(to - n - j));
+                }
+            }
+        }
+    }
+    if (end > 0) atomicMax(&last[k], end);
+    __syncthreads();
+    if (A.lengths && threadIdx.x < K) ((Global<int32_t>)A.lengths)[first + threadIdx.x] = last[threadIdx.x];
 }
 
 }  // namespace
@@ -796,10 +877,11 @@ void launch_beam_select(const BeamSelect& A, hipStream_t stream) {
 }
 
 void launch_batch_reorder(const BatchDev& D, uint32_t beams, const int32_t* parents_dev, int32_t* status_dev, hipStream_t stream) {
-    if (D.B == 0 || D.KF > 64) return;
+    static_assert(kSlotItems == 64 && kSlotSets + 1 >= 64 && kSlotWaits >= 64 && kSlotPlanes <= 64, "a wavefront asks for the first 64 of everything");
+    if (D.B == 0) return;
     const dim3 grid(D.B / beams), block(64 * std::min<uint32_t>(beams, 16));
-    if (beams <= 16) hipLaunchKernelGGL(k_batch_reorder<1>, grid, block, 0, stream, D, beams, parents_dev, status_dev);
-    else hipLaunchKernelGGL(k_batch_reorder<4>, grid, block, 0, stream, D, beams, parents_dev, status_dev);
+    if (beams <= 16) hipLaunchKernelGGL(k_batch_reorder<1>, grid, block, 0, stream, parents_dev, D.rows, beams, D, status_dev);
+    else hipLaunchKernelGGL(k_batch_reorder<4>, grid, block, 0, stream, parents_dev, D.rows, beams, D, status_dev);
 }
 
 template <class T, int MOST>
@@ -820,9 +902,22 @@ void launch_beam_reorder_rows(const BeamRows& A, hipStream_t stream) {
     else launch_rows_as<Wide2, 64>(A, stream);
 }
 
+template <int WIDTH>
+static void launch_backtrace_as(const BeamTrace& A, hipStream_t stream) {
+    // As many segments as a workgroup has room for, of eight steps at the least
+    constexpr uint32_t most = kTraceThreads / WIDTH;
+    const uint32_t length = std::max<uint32_t>(8, (A.steps + most - 1) / most), segments = (A.steps + length - 1) / length;
+    const uint32_t threads = std::max<uint32_t>(64, (segments * WIDTH + 63) / 64 * 64);
+    hipLaunchKernelGGL(k_beam_backtrace<WIDTH>, dim3(A.groups), dim3(threads), 0, stream, A, segments, length);
+}
+
 void launch_beam_backtrace(const BeamTrace& A, hipStream_t stream) {
     if (A.groups == 0) return;
-    hipLaunchKernelGGL(k_beam_backtrace, dim3(A.groups), dim3(64), 0, stream, A);
+    if (A.beams <= 4) launch_backtrace_as<4>(A, stream);
+    else if (A.beams <= 8) launch_backtrace_as<8>(A, stream);
+    else if (A.beams <= 16) launch_backtrace_as<16>(A, stream);
+    else if (A.beams <= 32) launch_backtrace_as<32>(A, stream);
+    else launch_backtrace_as<64>(A, stream);
 }
 
 }  // namespace xg2
