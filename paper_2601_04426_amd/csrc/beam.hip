@@ -76,6 +76,9 @@ constexpr float LOG2E = 1.44269504088896340736f;
 constexpr double LN2 = 0.693147180559945309417232;
 
 typedef uint32_t Vec4 __attribute__((ext_vector_type(4)));
+// vectors at any byte: the device takes them
+typedef uint32_t Wide4 __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t Wide2 __attribute__((ext_vector_type(2), aligned(1)));
 template <class E> struct Elem;
 template <> struct Elem<float> {
     static constexpr int EPV = 4;
@@ -107,20 +110,23 @@ __device__ __forceinline__ Vec4 stats_of(float top, float sum, float best) { ret
 template <class E> __device__ __forceinline__ int before_row(const E* row) { return (int)(reinterpret_cast<uintptr_t>(row) & 127) / (int)sizeof(E); }
 
 // A row whose beam has ended or does not exist is not read.
-__device__ __forceinline__ bool live_row(const BeamSelect& A, uint32_t r) {
-    const float s = A.scores[r];
-    return !(A.finished && A.finished[r] != 0) && s > NINF && s < -NINF;
+__device__ __forceinline__ bool live_row(const float* scores, const int32_t* finished, uint32_t r) {
+    const float s = ((Global<const float>)scores)[r];
+    const int32_t ended = finished ? ((Global<const int32_t>)finished)[r] : 0;
+    return ended == 0 && s > NINF && s < -NINF;
 }
 
 // WHICH: 0 no mask, 1 the softmax goes over the allowed tokens, 2 over all.
 template <class E, int WHICH>
-__global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(BeamSelect A, uint32_t first_row) {
+__global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* bitmask, long long bm_stride, const float* scores, const int32_t* finished,
+                                                                const void* logits, long long row_stride, uint32_t pieces, int V, BeamSelect A, uint32_t first_row) {
+    // (the first 14 words of arguments are in registers when the kernel starts, a struct's are loaded)
     constexpr int EPV = Elem<E>::EPV, STEPS = kBeamPiece / 64 / EPV, VPW = 32 / EPV;   // vectors of a mask word
     constexpr uint32_t ALL = (1u << EPV) - 1;
     const uint32_t r = first_row + blockIdx.y, lane = threadIdx.x & 63, piece = blockIdx.x * (blockDim.x >> 6) + uniform(threadIdx.x >> 6);
-    if (piece >= A.pieces || !live_row(A, r)) return;
-    const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
-    const int V = A.V, e0 = (int)piece * kBeamPiece - before_row(row);             // (V is at most 2^30)
+    if (piece >= pieces) return;
+    const E* const row = static_cast<const E*>(logits) + (long long)r * row_stride;
+    const int e0 = (int)piece * kBeamPiece - before_row(row);             // (V is at most 2^30)
     const bool inner = e0 >= 0 && e0 + kBeamPiece <= V;
     // this lane's 32 tokens from e0 + 32 * lane on: which are in the row, and which of them are allowed
     const int first = e0 + 32 * (int)lane;
@@ -131,18 +137,16 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(BeamSelect A, uin
     }
     uint32_t allowed = inside;
     if (WHICH != 0) {
-        const Global<const uint32_t> bm = (Global<const uint32_t>)(A.bitmask + (long long)r * A.bm_stride);
-        const int at = first >> 5, last = (V - 1) >> 5, shift = e0 & 31;            // (an arithmetic shift: rounds down; shift is the same in all lanes)
-        uint32_t word = at >= 0 && at <= last ? bm[at] : 0;
-        if (shift != 0) {
-            const uint32_t next = at + 1 >= 0 && at + 1 <= last ? bm[at + 1] : 0;
-            word = (word >> shift) | (next << (32 - shift));
-        }
-        allowed &= word;
+        // (of words that are not the row's any: their tokens are not inside)
+        const Global<const uint32_t> bm = (Global<const uint32_t>)(bitmask + (long long)r * bm_stride);
+        const int at = first >> 5, last = (V - 1) >> 5;                              // (an arithmetic shift: rounds down)
+        const uint32_t word = bm[min(max(at, 0), last)], next = bm[min(max(at + 1, 0), last)];
+        allowed &= (uint32_t)(((uint64_t)next << 32 | word) >> (e0 & 31));
     }
+    if (!live_row(scores, finished, r)) return;
     const uint32_t counted = WHICH == 1 ? allowed : inside;
-    const Global<Vec4> stats = (Global<Vec4>)(A.stats + ((size_t)r * A.pieces + piece));
-    const Global<float> block_max = (Global<float>)(A.block_max + ((size_t)r * A.pieces + piece) * kBeamPieceBlocks);
+    const Global<Vec4> stats = (Global<Vec4>)(A.stats + ((size_t)r * pieces + piece));
+    const Global<float> block_max = (Global<float>)(A.block_max + ((size_t)r * pieces + piece) * kBeamPieceBlocks);
     if (WHICH == 1 && __ballot(counted != 0) == 0) {
         if (lane == 0) *stats = stats_of(NINF, 0.f, NINF);
         if (lane < kBeamPieceBlocks) block_max[lane] = NINF;
@@ -158,7 +162,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(BeamSelect A, uin
         _Pragma("unroll") for (int j = 0; j < STEPS; ++j) bits[j] = ((uint32_t)__shfl((int)counted, (j * 64 + (int)lane) / VPW) >> ((int)lane % VPW * EPV)) & ALL;
         // A vector that the row shares with its neighbours lies between the buffer's first and last logit all the same, but for one at the
         // begin of the first row and one at the end of the last: these are put together from logits.
-        const long long at = (long long)r * A.row_stride + e0, end = (long long)(A.groups * A.beams - 1) * A.row_stride + V;
+        const long long at = (long long)r * row_stride + e0, end = (long long)(A.groups * A.beams - 1) * row_stride + V;
         const bool apart = !inner && (at < 0 || at + kBeamPiece > end);
         unsigned long long open = 0;
         _Pragma("unroll") for (int j = 0; j < STEPS; ++j) {
@@ -324,43 +328,75 @@ __device__ __forceinline__ bool token_allowed(const BeamSelect& A, uint32_t r, l
 __device__ __forceinline__ uint64_t place_of(uint32_t row, long long token) { return (uint64_t)row << 32 | (uint64_t)(token + 1); }
 __device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) { return a.score > b.score || (a.score == b.score && a.at < b.at); }
 
-// The row's sum in 64 bits, and the maxima of its pieces and blocks without NaN: what the first kernel left of the row is not used.
+// 16 tokens of a row from t0 on: their logits, and which of them are in the row and, unless all
+// are wanted, allowed.
 template <class E>
-__device__ __attribute__((noinline)) void repair_row(const BeamSelect& A, PickShared& S, uint32_t g, uint32_t k) {
+__device__ __forceinline__ uint32_t load_16(const BeamSelect& A, uint32_t r, int t0, bool all, float* x) {
+    constexpr int EPV = Elem<E>::EPV, VECS = 16 / EPV;
+    const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
+    const bool inner = t0 >= 0 && t0 + 16 <= A.V;
+    Vec4 raw[VECS];
+    uint32_t ok = 0xFFFF;
+    if (A.bitmask && !all) {
+        const Global<const uint32_t> bm = (Global<const uint32_t>)(A.bitmask + (long long)r * A.bm_stride);
+        const int at = t0 >> 5, last = (A.V - 1) >> 5;               // (an arithmetic shift: rounds down)
+        ok = (uint32_t)(((uint64_t)bm[min(max(at + 1, 0), last)] << 32 | bm[min(max(at, 0), last)]) >> (t0 & 31));
+    }
+    if (inner) { _Pragma("unroll") for (int v = 0; v < VECS; ++v) raw[v] = ((Global<const Wide4>)(row + t0))[v]; }
+    else {
+        _Pragma("unroll") for (int v = 0; v < VECS; ++v) raw[v] = Elem<E>::gather(row, t0 + v * EPV, A.V);
+        if (t0 < 0) ok &= 0xFFFFu << min(-t0, 16);
+        if (t0 + 16 > A.V) ok &= t0 < A.V ? 0xFFFFu >> (t0 + 16 - A.V) : 0u;
+    }
+    _Pragma("unroll") for (int v = 0; v < VECS; ++v) Elem<E>::unpack(raw[v], x + v * EPV);
+    return ok & 0xFFFF;
+}
+
+// The row's sum in 64 bits; anew: also the maxima of its pieces and blocks without NaN (what the first kernel left of the row is not used).
+template <class E>
+__device__ __attribute__((noinline)) void repair_row(const BeamSelect& A, PickShared& S, uint32_t g, uint32_t k, bool anew) {
     const uint32_t r = g * A.beams + k, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x >> 6;
     const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
-    float top = NINF;
+    const int before = before_row(row);
+    float top = NINF, x[16];
     __syncthreads();                                                 // (S.wave_top has been read by all)
-    for (uint32_t p = wave; p < A.pieces; p += waves) {
-        float piece_best = NINF;
-        for (int b = 0; b < kBeamPieceBlocks; ++b) {
-            const int t0 = (int)p * kBeamPiece + b * kBeamBlock - before_row(row);
-            float best = NINF;
-            for (int c = 0; c < kBeamBlock; c += 64) {
-                const int t = t0 + c + (int)lane;
-                if (t < 0 || t >= A.V) continue;
-                const float x = Elem<E>::load(row + t);
-                const bool ok = token_allowed(A, r, t);
-                if (ok) best = x > best ? x : best;                  // (false for NaN)
-                if (ok || A.over_all) top = x > top ? x : top;
+    if (anew) {
+        // 16 lanes have a block, and in eight turns a piece
+        for (uint32_t p = tid >> 4; p < A.pieces; p += blockDim.x >> 4) {
+            float piece_best = NINF;
+            for (int b = 0; b < kBeamPieceBlocks; ++b) {
+                const int t0 = (int)p * kBeamPiece + b * kBeamBlock + 16 * (int)(tid & 15) - before;
+                const uint32_t inside = load_16<E>(A, r, t0, true, x);
+                uint32_t ok = inside;
+                if (A.bitmask) { float again[16]; ok = load_16<E>(A, r, t0, false, again); }
+                float best = NINF;
+                for (int c = 0; c < 16; ++c) {
+                    if ((ok >> c) & 1u) best = x[c] > best ? x[c] : best;                                    // (false for NaN)
+                    if (((A.over_all ? inside : ok) >> c) & 1u) top = x[c] > top ? x[c] : top;
+                }
+                best = largest_of_16(best);
+                if ((tid & 15) == 0) ((Global<float>)A.block_max)[((size_t)r * A.pieces + p) * kBeamPieceBlocks + b] = best;
+                piece_best = best > piece_best ? best : piece_best;
             }
-            for (int d = 1; d < 64; d *= 2) { const float o = __shfl_xor(best, d); best = o > best ? o : best; }
-            if (lane == 0) ((Global<float>)A.block_max)[((size_t)r * A.pieces + p) * kBeamPieceBlocks + b] = best;
-            piece_best = best > piece_best ? best : piece_best;
+            if ((tid & 15) == 0) ((Global<float>)(A.stats + ((size_t)r * A.pieces + p)))[2] = piece_best;
         }
-        if (lane == 0) ((Global<float>)(A.stats + ((size_t)r * A.pieces + p)))[2] = piece_best;
+    } else {
+        for (uint32_t p = tid; p < A.pieces; p += blockDim.x) { const float o = ((Global<const float>)(A.stats + ((size_t)r * A.pieces + p)))[0]; top = o > top ? o : top; }
     }
     for (int d = 1; d < 64; d *= 2) { const float o = __shfl_xor(top, d); top = o > top ? o : top; }
     if (lane == 0) S.wave_top[wave] = top;
     __syncthreads();
     for (uint32_t w = 0; w < waves; ++w) top = (float)S.wave_top[w] > top ? (float)S.wave_top[w] : top;
     __syncthreads();
+    // (counted from the row's begin, wherever it lies: rows that are alike have sums that are alike)
     double sum = 0;
-    for (int t = (int)tid; t < A.V; t += (int)blockDim.x) {
-        const float x = Elem<E>::load(row + t);
-        if (!(x > NINF) || !(A.over_all || token_allowed(A, r, t))) continue;
-        if (top == -NINF) sum += x == top ? 1.0 : 0.0;
-        else sum += exp((double)x - (double)top);
+    for (int t0 = 16 * (int)tid; t0 < A.V; t0 += 16 * (int)blockDim.x) {
+        uint32_t ok = load_16<E>(A, r, t0, A.over_all, x);
+        if (ok == 0) continue;
+        _Pragma("unroll 4") for (int c = 0; c < 16; ++c) {
+            const double e = top == -NINF ? (x[c] == top ? 1.0 : 0.0) : exp((double)x[c] - (double)top);
+            sum += ((ok >> c) & 1u) && x[c] > NINF ? e : 0.0;
+        }
     }
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     if (lane == 0) S.wave_top[wave] = sum;
@@ -410,7 +446,7 @@ template <class E>
 __device__ __attribute__((noinline)) void pick_one_by_one(const BeamSelect& A, PickShared& S, uint32_t g) {
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6, K = A.beams, N = A.n_out, n_blocks = A.pieces * kBeamPieceBlocks;
     const double none = -(double)__builtin_inff();
-    for (uint32_t k = 0; k < K; ++k) if (S.state[k] == ROW_LIVE && !S.exact[k]) repair_row<E>(A, S, g, k);
+    for (uint32_t k = 0; k < K; ++k) if (S.state[k] == ROW_LIVE && !S.exact[k]) repair_row<E>(A, S, g, k, false);
     uint32_t n_found = 0;
     Candidate last{0, ~0ull};
     for (; n_found < N; ++n_found) {
@@ -454,21 +490,21 @@ __device__ __attribute__((noinline)) void pick_one_by_one(const BeamSelect& A, P
 }
 
 template <class E>
-__global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamSelect A) {
+__global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_stats, const float* scores, const int32_t* finished, uint32_t K, uint32_t pieces, uint32_t N, BeamSelect A) {
     __shared__ PickShared S;
-    const uint32_t g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x >> 6, K = A.beams, N = A.n_out, pieces = A.pieces;
+    const uint32_t g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x >> 6;
     constexpr double none = -(double)__builtin_inff();
     // 16 lanes of a row: the row's sum
     const uint32_t k = tid >> 4, part = tid & 15, r = g * K + k;
-    const Global<const Vec4> stats = (Global<const Vec4>)(A.stats + (size_t)r * pieces);
+    const Global<const Vec4> stats = (Global<const Vec4>)(all_stats + (size_t)r * pieces);
     const bool mine = k < K;
     float s = NINF, best[kPickHeld];
     Vec4 held[kPickHeld];
     bool ended = false;
     if (mine) {
         _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) held[i] = stats[min(part + i * 16, pieces - 1)];
-        s = ((Global<const float>)A.scores)[r];
-        if (A.finished) ended = ((Global<const int32_t>)A.finished)[r] != 0;
+        s = ((Global<const float>)scores)[r];
+        if (finished) ended = ((Global<const int32_t>)finished)[r] != 0;
     }
     for (uint32_t i = tid; i < kPickBins; i += blockDim.x) S.bins[i] = 0;
     if (tid == 0) S.n_pieces = S.n_blocks = S.n_elems = 0;
@@ -516,7 +552,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamSelect A) {
     }
     if (lane == 0) S.wave_top[wave] = top;
     if (__syncthreads_or((int)repair)) {
-        for (uint32_t q = 0; q < K; ++q) if (S.repair[q]) repair_row<E>(A, S, g, q);
+        for (uint32_t q = 0; q < K; ++q) if (S.repair[q]) repair_row<E>(A, S, g, q, true);
         top = none;
         if (mine) {
             state = S.state[k];
@@ -581,27 +617,10 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamSelect A) {
     const uint32_t listed = min(S.n_blocks, (uint32_t)kPickListed);
     const double reach = last_bin < kPickBins - 1 ? top - reach_of(last_bin) : none;
     for (uint32_t i = tid >> 4; i < listed; i += blockDim.x >> 4) {
-        constexpr int EPV = Elem<E>::EPV, VECS = 16 / EPV;
         const uint32_t block = S.blocks[i], row_k = block >> kRowShift, row_r = g * K + row_k;
-        const E* const row = static_cast<const E*>(A.logits) + (long long)row_r * A.row_stride;
-        const int t0 = (int)((block & kRowBits) * kBeamBlock + 16 * part) - before_row(row);
-        const bool inner = t0 >= 0 && t0 + 16 <= A.V;
-        Vec4 raw[VECS];
-        uint32_t ok = 0xFFFF;
-        if (A.bitmask) {
-            const Global<const uint32_t> bm = (Global<const uint32_t>)(A.bitmask + (long long)row_r * A.bm_stride);
-            const uint64_t both = (uint64_t)bm[min(max(t0 + 15, 0), A.V - 1) >> 5] << 32 | bm[min(max(t0, 0), A.V - 1) >> 5];
-            const bool next = (max(t0, 0) & 31) + 16 > 32;           // (of a word that is its own neighbour the lower half is read)
-            ok = t0 >= 0 ? (uint32_t)((next ? both : both & 0xFFFFFFFFu) >> (t0 & 31)) : (uint32_t)both << min(-t0, 16);
-        }
-        if (inner) { _Pragma("unroll") for (int v = 0; v < VECS; ++v) raw[v] = ((Global<const Vec4>)(row + t0))[v]; }
-        else {
-            _Pragma("unroll") for (int v = 0; v < VECS; ++v) raw[v] = Elem<E>::gather(row, t0 + v * EPV, A.V);
-            if (t0 < 0) ok &= 0xFFFFu << min(-t0, 16);
-            if (t0 + 16 > A.V) ok &= t0 < A.V ? 0xFFFFu >> (t0 + 16 - A.V) : 0u;
-        }
+        const int t0 = (int)((block & kRowBits) * kBeamBlock + 16 * part) - before_row(static_cast<const E*>(A.logits) + (long long)row_r * A.row_stride);
         float x[16];
-        _Pragma("unroll") for (int v = 0; v < VECS; ++v) Elem<E>::unpack(raw[v], x + v * EPV);
+        const uint32_t ok = load_16<E>(A, row_r, t0, false, x);
         // a bound in 32 bits first
         const double least = reach - S.base[row_k];
         const float bound = (float)least - (__builtin_fabsf((float)least) * 1e-6f + 1e-3f);
@@ -621,25 +640,16 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamSelect A) {
     const uint32_t R = S.n_elems;
     for (;;) {
         // A candidate's place is the number of candidates before it: a wavefront compares 64 candidates with its part of all.
-        if (R <= 64) {
-            if (wave == 0) {
-                const Candidate c = S.found[lane < R ? lane : 0];
-                uint32_t n = 0;
-                _Pragma("unroll 4") for (uint32_t j = 0; j < R; ++j) n += before(S.found[j], c) ? 1u : 0u;
-                if (lane < R) S.sorted[n] = (uint16_t)lane;
-            }
-        } else {
-            const uint32_t chunks = (R + 63) / 64, parts = max(waves / chunks, 1u);
-            for (uint32_t w = wave; w < chunks * parts; w += waves) {
-                const uint32_t i = w % chunks * 64 + lane, p = w / chunks, to = (p + 1) * R / parts;
-                const Candidate c = S.found[i < R ? i : 0];
-                uint32_t n = 0;
-                _Pragma("unroll 4") for (uint32_t j = p * R / parts; j < to; ++j) n += before(S.found[j], c) ? 1u : 0u;
-                if (i < R && n != 0) atomicAdd(&S.place[i], n);
-            }
-            __syncthreads();
-            for (uint32_t i = tid; i < R; i += blockDim.x) { S.sorted[S.place[i]] = (uint16_t)i; S.place[i] = 0; }
+        const uint32_t chunks = (R + 63) / 64, parts = chunks == 0 ? 0 : max(waves / chunks, 1u);
+        for (uint32_t w = wave; w < chunks * parts; w += waves) {
+            const uint32_t i = w % chunks * 64 + lane, p = w / chunks, to = (p + 1) * R / parts;
+            const Candidate c = S.found[i < R ? i : 0];
+            uint32_t n = 0;
+            _Pragma("unroll 4") for (uint32_t j = p * R / parts; j < to; ++j) n += before(S.found[j], c) ? 1u : 0u;
+            if (i < R && n != 0) atomicAdd(&S.place[i], n);
         }
+        __syncthreads();
+        for (uint32_t i = tid; i < R; i += blockDim.x) { S.sorted[S.place[i]] = (uint16_t)i; S.place[i] = 0; }
         if (tid < K) S.repair[tid] = 0;
         __syncthreads();
         // Neighbours of different rows that are too close for their sums, among the chosen and those that are as close to the last of
@@ -652,7 +662,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamSelect A) {
             if (n + 1 <= N || !(S.found[S.sorted[N - 1]].score - b.score > A.near)) { S.repair[ka] = S.repair[kb] = 1; any = 1; }
         }
         if (!__syncthreads_or(any)) break;
-        for (uint32_t q = 0; q < K; ++q) if (S.repair[q] && !S.exact[q]) repair_row<E>(A, S, g, q);
+        for (uint32_t q = 0; q < K; ++q) if (S.repair[q] && !S.exact[q]) repair_row<E>(A, S, g, q, false);
         for (uint32_t i = tid; i < R; i += blockDim.x)
             if ((uint32_t)S.found[i].at != 0) S.found[i].score = score_of(S, (uint32_t)(S.found[i].at >> 32), S.x[i]);
         __syncthreads();
@@ -725,10 +735,6 @@ __global__ __launch_bounds__(1024) void k_batch_reorder(const int32_t* parents, 
 // ---- rows of a buffer -----------------------------------------------------------------------------------------------
 // A thread has one column of all rows of a group: it loads what every row will hold there and then stores it, so nothing waits for
 // anybody and no second buffer is needed.  Rows that keep their place are neither read (but as parents) nor written.
-// (vectors at any byte: the device takes them, and a row's stride or a position's size need not be a multiple of anything)
-typedef uint32_t Wide4 __attribute__((ext_vector_type(4), aligned(1)));
-typedef uint32_t Wide2 __attribute__((ext_vector_type(2), aligned(1)));
-
 template <class T, int MOST>
 __device__ __forceinline__ void move_column(uint8_t* at, int64_t row_stride, const int32_t* from, uint64_t moves) {
     T v[MOST];
@@ -864,10 +870,10 @@ static void launch_beam_select_as(const BeamSelect& A, hipStream_t stream) {
     const uint32_t waves = (uint64_t)A.pieces * rows <= 512 ? 1 : kScanWaves;
     for (uint32_t first = 0; first < rows; first += 65535) {         // grid.y limit
         const uint32_t n = std::min<uint32_t>(65535, rows - first);
-        hipLaunchKernelGGL(kernel, dim3((A.pieces + waves - 1) / waves, n), dim3(64 * waves), 0, stream, A, first);
+        hipLaunchKernelGGL(kernel, dim3((A.pieces + waves - 1) / waves, n), dim3(64 * waves), 0, stream, A.bitmask, A.bm_stride, A.scores, A.finished, A.logits, A.row_stride, A.pieces, A.V, A, first);
     }
     const uint32_t threads = std::min<uint32_t>(kPickThreads, std::max<uint32_t>(256, (16 * std::max(A.beams, A.n_out + A.n_out / 2) + 63) / 64 * 64));
-    hipLaunchKernelGGL(k_beam_pick<E>, dim3(A.groups), dim3(threads), 0, stream, A);
+    hipLaunchKernelGGL(k_beam_pick<E>, dim3(A.groups), dim3(threads), 0, stream, A.stats, A.scores, A.finished, A.beams, A.pieces, A.n_out, A);
 }
 
 void launch_beam_select(const BeamSelect& A, hipStream_t stream) {
