@@ -44,17 +44,24 @@ __device__ __forceinline__ float larger(float a, float b, float c) { float d; as
 // not wait for, and of which the compiler knows nothing here).
 #if defined(__HIP_DEVICE_COMPILE__)
 #define XG2_MAX4(HOW) "v_max_f32_dpp %0, %0, %0 " HOW "\n\tv_max_f32_dpp %1, %1, %1 " HOW "\n\tv_max_f32_dpp %2, %2, %2 " HOW "\n\tv_max_f32_dpp %3, %3, %3 " HOW "\n\t"
-#define XG2_MAX4_16 "s_nop 1\n\t" XG2_MAX4("quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf") XG2_MAX4("quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf") \
-    XG2_MAX4("row_half_mirror row_mask:0xf bank_mask:0xf") XG2_MAX4("row_mirror row_mask:0xf bank_mask:0xf")
-__device__ __forceinline__ void largest_of_32(float& a, float& b, float& c, float& d) {                                                     // lanes 31, 63
-    asm volatile(XG2_MAX4_16 XG2_MAX4("row_bcast:15 row_mask:0xa bank_mask:0xf") "s_nop 1" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+__device__ __forceinline__ void largest_of_8(float& a, float& b, float& c, float& d) {                                                      // all lanes
+    asm volatile("s_nop 1\n\t" XG2_MAX4("quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf") XG2_MAX4("quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf")
+                 XG2_MAX4("row_half_mirror row_mask:0xf bank_mask:0xf") "s_nop 1" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
 }
-__device__ __forceinline__ void largest_of_64(float& a, float& b, float& c, float& d) {                                                     // lane 63
-    asm volatile(XG2_MAX4_16 XG2_MAX4("row_bcast:15 row_mask:0xa bank_mask:0xf") XG2_MAX4("row_bcast:31 row_mask:0xc bank_mask:0xf") "s_nop 1" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+__device__ __forceinline__ void largest_of_16(float& a, float& b, float& c, float& d) {                                                     // all lanes
+    asm volatile("s_nop 1\n\t" XG2_MAX4("quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf") XG2_MAX4("quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf")
+                 XG2_MAX4("row_half_mirror row_mask:0xf bank_mask:0xf") XG2_MAX4("row_mirror row_mask:0xf bank_mask:0xf") "s_nop 1" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+}
+__device__ __forceinline__ float largest_of_64(float v) {                                                                                  // lane 63
+    asm volatile("s_nop 1\n\tv_max_f32_dpp %0, %0, %0 quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\ts_nop 1\n\tv_max_f32_dpp %0, %0, %0 quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+                 "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_half_mirror row_mask:0xf bank_mask:0xf\n\ts_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_mirror row_mask:0xf bank_mask:0xf\n\t"
+                 "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_bcast:15 row_mask:0xa bank_mask:0xf\n\ts_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_bcast:31 row_mask:0xc bank_mask:0xf\n\ts_nop 1" : "+v"(v));
+    return v;
 }
 #else
-__device__ void largest_of_32(float&, float&, float&, float&) {}
-__device__ void largest_of_64(float&, float&, float&, float&) {}
+__device__ void largest_of_8(float&, float&, float&, float&) {}
+__device__ void largest_of_16(float&, float&, float&, float&) {}
+__device__ float largest_of_64(float v) { return v; }
 #endif
 __device__ __forceinline__ float sum_of_64(float v) {                                                                                      // lane 63
     v += moved<DPP_SWAP1>(v, v);
@@ -121,7 +128,7 @@ template <class E, int WHICH>
 __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* bitmask, long long bm_stride, const float* scores, const int32_t* finished,
                                                                 const void* logits, long long row_stride, uint32_t pieces, int V, BeamSelect A, uint32_t first_row) {
     // (the first 14 words of arguments are in registers when the kernel starts, a struct's are loaded)
-    constexpr int EPV = Elem<E>::EPV, STEPS = kBeamPiece / 64 / EPV, VPW = 32 / EPV;   // vectors of a mask word
+    constexpr int EPV = Elem<E>::EPV, STEPS = kBeamPiece / 64 / EPV, VPW = 32 / EPV, LANES = kBeamBlock / EPV;   // vectors of a mask word, lanes of a block
     constexpr uint32_t ALL = (1u << EPV) - 1;
     const uint32_t r = first_row + blockIdx.y, lane = threadIdx.x & 63, piece = blockIdx.x * (blockDim.x >> 6) + uniform(threadIdx.x >> 6);
     if (piece >= pieces) return;
@@ -149,7 +156,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
     const Global<float> block_max = (Global<float>)(A.block_max + ((size_t)r * pieces + piece) * kBeamPieceBlocks);
     if (WHICH == 1 && __ballot(counted != 0) == 0) {
         if (lane == 0) *stats = stats_of(NINF, 0.f, NINF);
-        if (lane < kBeamPieceBlocks) block_max[lane] = NINF;
+        if (lane < kBeamPieceBlocks) block_max[lane] = NINF;                           // (a wavefront has as many lanes)
         return;
     }
     const E* const from = row + e0;
@@ -193,7 +200,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
         float m = larger(x[j][0], x[j][1], x[j][2]);
         if (EPV == 8) { m = larger(m, x[j][3], x[j][4]); m = larger(m, x[j][5], x[j][6]); }
         m = larger(m, x[j][EPV - 1]);
-        top = larger(top, m);
+        if (WHICH == 2) top = larger(top, m);
         if (WHICH == 2) {
             const uint32_t ok = (uint32_t)__shfl((int)allowed, (j * 64 + (int)lane) / VPW) >> ((int)lane % VPW * EPV);
             float y[EPV];
@@ -207,27 +214,17 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
         }
         best[j] = m;
     }
-    if (EPV == 8) largest_of_32(best[0], best[1], best[2], best[3]);
-    else { _Pragma("unroll") for (int j = 0; j < STEPS; j += 4) largest_of_64(best[j], best[j + 1], best[j + 2], best[j + 3]); }
+    // the largest logit a lane has, then a block's maximum in all its lanes, of which the j-th writes that of step j
+    float own = best[0];
+    _Pragma("unroll") for (int j = 1; j < STEPS; ++j) own = larger(own, best[j]);
+    if (EPV == 8) largest_of_8(best[0], best[1], best[2], best[3]);
+    else { _Pragma("unroll") for (int j = 0; j < STEPS; j += 4) largest_of_16(best[j], best[j + 1], best[j + 2], best[j + 3]); }
+    const uint32_t turn = lane % LANES;
+    float written = best[0];
+    _Pragma("unroll") for (int j = 1; j < STEPS; ++j) written = turn == (uint32_t)j ? best[j] : written;
+    if (turn < STEPS) block_max[turn * (64 / LANES) + lane / LANES] = written;
     // the piece's largest allowed logit, and its largest that counts
-    float ok_max = best[0];
-    _Pragma("unroll") for (int j = 1; j < STEPS; ++j) ok_max = larger(ok_max, best[j]);
-    READABLE(ok_max);
-    ok_max = EPV == 8 ? larger(lane_float(ok_max, 31), lane_float(ok_max, 63)) : lane_float(ok_max, 63);
-    float all = ok_max;
-    if (WHICH == 2) {
-        float same = top, same2 = top, same3 = top;
-        largest_of_64(top, same, same2, same3);
-        all = lane_float(top, 63);
-    }
-    if (EPV == 8) {
-        if ((lane & 31) == 31) { _Pragma("unroll") for (int j = 0; j < STEPS; ++j) block_max[2 * j + (lane >> 5)] = best[j]; }
-    } else if (lane == 63) {
-        Vec4 b[2];
-        _Pragma("unroll") for (int j = 0; j < STEPS; ++j) b[j / 4][j % 4] = __float_as_uint(best[j]);
-        ((Global<Vec4>)block_max)[0] = b[0];
-        ((Global<Vec4>)block_max)[1] = b[1];
-    }
+    const float ok_max = lane_float(largest_of_64(own), 63), all = WHICH == 2 ? lane_float(largest_of_64(top), 63) : ok_max;
     float sum = 0;
     if (all > NINF) {
         const float c = larger(__fmul_rn(all, LOG2E), -3.4028234e38f);             // (finite, or minus infinity would come back as NaN)
@@ -361,11 +358,11 @@ __device__ __attribute__((noinline)) void repair_row(const BeamSelect& A, PickSh
     float top = NINF, x[16];
     __syncthreads();                                                 // (S.wave_top has been read by all)
     if (anew) {
-        // 16 lanes have a block, and in eight turns a piece
-        for (uint32_t p = tid >> 4; p < A.pieces; p += blockDim.x >> 4) {
+        // four lanes have a block, a wavefront in two turns a piece
+        for (uint32_t p = wave; p < A.pieces; p += waves) {
             float piece_best = NINF;
-            for (int b = 0; b < kBeamPieceBlocks; ++b) {
-                const int t0 = (int)p * kBeamPiece + b * kBeamBlock + 16 * (int)(tid & 15) - before;
+            for (uint32_t b = lane >> 2; b < kBeamPieceBlocks; b += 16) {
+                const int t0 = (int)p * kBeamPiece + (int)b * kBeamBlock + 16 * (int)(lane & 3) - before;
                 const uint32_t inside = load_16<E>(A, r, t0, true, x);
                 uint32_t ok = inside;
                 if (A.bitmask) { float again[16]; ok = load_16<E>(A, r, t0, false, again); }
@@ -374,11 +371,12 @@ __device__ __attribute__((noinline)) void repair_row(const BeamSelect& A, PickSh
                     if ((ok >> c) & 1u) best = x[c] > best ? x[c] : best;                                    // (false for NaN)
                     if (((A.over_all ? inside : ok) >> c) & 1u) top = x[c] > top ? x[c] : top;
                 }
-                best = largest_of_16(best);
-                if ((tid & 15) == 0) ((Global<float>)A.block_max)[((size_t)r * A.pieces + p) * kBeamPieceBlocks + b] = best;
+                for (int d = 1; d < 4; d *= 2) { const float o = __shfl_xor(best, d); best = o > best ? o : best; }
+                if ((lane & 3) == 0) ((Global<float>)A.block_max)[((size_t)r * A.pieces + p) * kBeamPieceBlocks + b] = best;
                 piece_best = best > piece_best ? best : piece_best;
             }
-            if ((tid & 15) == 0) ((Global<float>)(A.stats + ((size_t)r * A.pieces + p)))[2] = piece_best;
+            for (int d = 4; d < 64; d *= 2) { const float o = __shfl_xor(piece_best, d); piece_best = o > piece_best ? o : piece_best; }
+            if (lane == 0) ((Global<float>)(A.stats + ((size_t)r * A.pieces + p)))[2] = piece_best;
         }
     } else {
         for (uint32_t p = tid; p < A.pieces; p += blockDim.x) { const float o = ((Global<const float>)(A.stats + ((size_t)r * A.pieces + p)))[0]; top = o > top ? o : top; }
@@ -605,20 +603,31 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
     } else if (state == ROW_ENDED && part == 0) list_candidate(S.base[k], place_of(k, -1), 0.f);
     __syncthreads();
     const uint32_t n_pieces = min(S.n_pieces, (uint32_t)kPickListed);
-    for (uint32_t i = tid; i < n_pieces * kBeamPieceBlocks; i += blockDim.x) {
-        const uint32_t piece = S.pieces[i / kBeamPieceBlocks], row_k = piece >> kRowShift, block = (piece & kRowBits) * kBeamPieceBlocks + i % kBeamPieceBlocks;
-        if (bin_if(row_k, ((Global<const float>)A.block_max)[(size_t)(g * K + row_k) * pieces * kBeamPieceBlocks + block]) > last_bin) continue;
-        const uint32_t at = atomicAdd(&S.n_blocks, 1u);
-        if (at < kPickListed) S.blocks[at] = row_k << kRowShift | block;
+    for (uint32_t i0 = tid; i0 < n_pieces * kBeamPieceBlocks; i0 += 4 * blockDim.x) {
+        uint32_t at[4];                                              // (four loads before the first is used)
+        float m[4];
+        _Pragma("unroll") for (int q = 0; q < 4; ++q) {
+            const uint32_t i = i0 + q * blockDim.x;
+            m[q] = NINF;
+            if (i >= n_pieces * kBeamPieceBlocks) continue;
+            const uint32_t piece = S.pieces[i / kBeamPieceBlocks], row_k = piece >> kRowShift, block = (piece & kRowBits) * kBeamPieceBlocks + i % kBeamPieceBlocks;
+            at[q] = row_k << kRowShift | block;
+            m[q] = ((Global<const float>)A.block_max)[(size_t)(g * K + row_k) * pieces * kBeamPieceBlocks + block];
+        }
+        _Pragma("unroll") for (int q = 0; q < 4; ++q) {
+            if (!(m[q] > NINF) || bin_if(at[q] >> kRowShift, m[q]) > last_bin) continue;
+            const uint32_t n = atomicAdd(&S.n_blocks, 1u);
+            if (n < kPickListed) S.blocks[n] = at[q];
+        }
     }
     for (uint32_t i = tid; i < kPickElems; i += blockDim.x) S.place[i] = 0;
     __syncthreads();
-    // 16 lanes have a block, each of them 16 tokens
+    // four lanes have a block, each of them 16 tokens
     const uint32_t listed = min(S.n_blocks, (uint32_t)kPickListed);
     const double reach = last_bin < kPickBins - 1 ? top - reach_of(last_bin) : none;
-    for (uint32_t i = tid >> 4; i < listed; i += blockDim.x >> 4) {
+    for (uint32_t i = tid >> 2; i < listed; i += blockDim.x >> 2) {
         const uint32_t block = S.blocks[i], row_k = block >> kRowShift, row_r = g * K + row_k;
-        const int t0 = (int)((block & kRowBits) * kBeamBlock + 16 * part) - before_row(static_cast<const E*>(A.logits) + (long long)row_r * A.row_stride);
+        const int t0 = (int)((block & kRowBits) * kBeamBlock + 16 * (tid & 3)) - before_row(static_cast<const E*>(A.logits) + (long long)row_r * A.row_stride);
         float x[16];
         const uint32_t ok = load_16<E>(A, row_r, t0, false, x);
         // a bound in 32 bits first
@@ -872,7 +881,7 @@ static void launch_beam_select_as(const BeamSelect& A, hipStream_t stream) {
         const uint32_t n = std::min<uint32_t>(65535, rows - first);
         hipLaunchKernelGGL(kernel, dim3((A.pieces + waves - 1) / waves, n), dim3(64 * waves), 0, stream, A.bitmask, A.bm_stride, A.scores, A.finished, A.logits, A.row_stride, A.pieces, A.V, A, first);
     }
-    const uint32_t threads = std::min<uint32_t>(kPickThreads, std::max<uint32_t>(256, (16 * std::max(A.beams, A.n_out + A.n_out / 2) + 63) / 64 * 64));
+    const uint32_t threads = std::min<uint32_t>(kPickThreads, std::max<uint32_t>(256, (std::max(16 * A.beams, 4 * (A.n_out + A.n_out / 4)) + 63) / 64 * 64));
     hipLaunchKernelGGL(k_beam_pick<E>, dim3(A.groups), dim3(threads), 0, stream, A.stats, A.scores, A.finished, A.beams, A.pieces, A.n_out, A);
 }
 

@@ -13,7 +13,7 @@ namespace xg2 {
 constexpr uint32_t kBeamsMost = 64, kBeamOutMost = 128;     // beams of a group; candidates chosen for one
 constexpr int32_t kBeamVocabMost = 1 << 30;
 constexpr uint32_t kBeamRowsMost = 1u << 20;
-constexpr int kBeamPiece = 2048, kBeamBlock = 256;          // tokens that a wavefront takes; tokens that share a maximum
+constexpr int kBeamPiece = 2048, kBeamBlock = 64;           // tokens that a wavefront takes; tokens that share a maximum
 constexpr int kBeamPieceBlocks = kBeamPiece / kBeamBlock;
 // Pieces of a row, counted from the 128-byte boundary at or before its begin, wherever that lies.
 constexpr uint32_t beam_pieces(int32_t V, int32_t elem_bytes) { return ((uint32_t)V + 128u / (uint32_t)elem_bytes - 1 + kBeamPiece - 1) / kBeamPiece; }
