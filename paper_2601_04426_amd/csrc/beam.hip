@@ -323,7 +323,8 @@ __device__ __forceinline__ bool token_allowed(const BeamSelect& A, uint32_t r, l
     return !A.bitmask || ((((Global<const uint32_t>)A.bitmask)[(long long)r * A.bm_stride + (t >> 5)] >> (t & 31)) & 1u);
 }
 __device__ __forceinline__ uint64_t place_of(uint32_t row, long long token) { return (uint64_t)row << 32 | (uint64_t)(token + 1); }
-__device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) { return a.score > b.score || (a.score == b.score && a.at < b.at); }
+// (no branch: three compares)
+__device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) { return (a.score > b.score) | ((a.score == b.score) & (a.at < b.at)); }
 
 // 16 tokens of a row from t0 on: their logits, and which of them are in the row and, unless all
 // are wanted, allowed.
@@ -649,12 +650,15 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
     const uint32_t R = S.n_elems;
     for (;;) {
         // A candidate's place is the number of candidates before it: a wavefront compares 64 candidates with its part of all.
-        const uint32_t chunks = (R + 63) / 64, parts = chunks == 0 ? 0 : max(waves / chunks, 1u);
-        for (uint32_t w = wave; w < chunks * parts; w += waves) {
-            const uint32_t i = w % chunks * 64 + lane, p = w / chunks, to = (p + 1) * R / parts;
+        // (16 of all for each, so that a few candidates take four wavefronts and no division)
+        const uint32_t sixteenths = (R + 15) / 16;
+        for (uint32_t i = lane; i < (R + 63) / 64 * 64; i += 64) {
             const Candidate c = S.found[i < R ? i : 0];
             uint32_t n = 0;
-            _Pragma("unroll 4") for (uint32_t j = p * R / parts; j < to; ++j) n += before(S.found[j], c) ? 1u : 0u;
+            for (uint32_t q = wave; q < sixteenths; q += waves) {
+                const uint32_t to = min(q * 16 + 16, R);
+                _Pragma("unroll 4") for (uint32_t j = q * 16; j < to; ++j) { const Candidate o = S.found[j]; n += before(o, c) ? 1u : 0u; }
+            }
             if (i < R && n != 0) atomicAdd(&S.place[i], n);
         }
         __syncthreads();
