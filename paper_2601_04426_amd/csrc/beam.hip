@@ -748,37 +748,30 @@ __global__ __launch_bounds__(1024) void k_batch_reorder(const int32_t* parents, 
 // ---- rows of a buffer -----------------------------------------------------------------------------------------------
 // A thread has one column of all rows of a group: it loads what every row will hold there and then stores it, so nothing waits for
 // anybody and no second buffer is needed.  Rows that keep their place are neither read (but as parents) nor written.
+// (from: lane k has the row that row k takes; the lane's rows are picked by constants)
 template <class T, int MOST>
-__device__ __forceinline__ void move_column(uint8_t* at, int64_t row_stride, const int32_t* from, uint64_t moves) {
+__device__ __forceinline__ void move_column(uint8_t* at, int64_t row_stride, uint32_t from, uint64_t moves) {
     T v[MOST];
 #pragma unroll
     for (int k = 0; k < MOST; ++k)
-        if ((moves >> k) & 1) v[k] = *reinterpret_cast<const T*>(at + (int64_t)uniform((uint32_t)from[k]) * row_stride);
+        if ((moves >> k) & 1) v[k] = *(Global<const T>)(at + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)from, k) * row_stride);
 #pragma unroll
     for (int k = 0; k < MOST; ++k)
-        if ((moves >> k) & 1) *reinterpret_cast<T*>(at + (int64_t)k * row_stride) = v[k];
+        if ((moves >> k) & 1) *(Global<T>)(at + (int64_t)k * row_stride) = v[k];
 }
 
 template <class T, int MOST>
-__global__ __launch_bounds__(256) void k_beam_reorder_rows(BeamRows A, uint32_t splits) {
-    __shared__ int32_t from[kBeamsMost];
-    __shared__ uint64_t moving;
-    const uint32_t split = blockIdx.x % splits, unit = blockIdx.x / splits, g = blockIdx.y + blockIdx.z * 32768u, K = A.beams;
+__global__ __launch_bounds__(256) void k_beam_reorder_rows(const int32_t* parents, const int32_t* begins, const int32_t* ends, uint32_t K, uint32_t splits, uint32_t positions, BeamRows A) {
+    const uint32_t split = blockIdx.x % splits, unit = blockIdx.x / splits, g = blockIdx.y + blockIdx.z * 32768u, lane = threadIdx.x & 63;
     if (g >= A.groups) return;
-    if (threadIdx.x < 64) {
-        const int32_t p = threadIdx.x < K ? A.parents[g * K + threadIdx.x] : -1, k = p >= 0 ? p - (int32_t)(g * K) : -1;
-        const bool moves = k >= 0 && k < (int32_t)K && k != (int32_t)threadIdx.x;
-        from[threadIdx.x] = moves ? k : 0;
-        const uint64_t all = __ballot(moves);
-        if (threadIdx.x == 0) moving = all;
-    }
-    __syncthreads();
-    const uint64_t moves = (uint64_t)uniform((uint32_t)(moving >> 32)) << 32 | uniform((uint32_t)moving);
-    if (moves == 0) return;
-    int64_t begin = A.begin ? A.begin[g] : 0, end = A.end ? A.end[g] : (int64_t)A.positions;
+    const int32_t p = lane < K ? ((Global<const int32_t>)parents)[g * K + lane] : -1;
+    int64_t begin = begins ? ((Global<const int32_t>)begins)[g] : 0, end = ends ? ((Global<const int32_t>)ends)[g] : (int64_t)positions;
     begin = begin < 0 ? 0 : begin;
-    end = end > (int64_t)A.positions ? (int64_t)A.positions : end;
+    end = end > (int64_t)positions ? (int64_t)positions : end;
     if (begin >= end) return;
+    const uint32_t from = (uint32_t)p - g * K;
+    const uint64_t moves = __ballot(p >= 0 && from < K && from != lane);
+    if (moves == 0) return;
     uint8_t* const piece = A.data + (int64_t)(g * K) * A.row_stride + (int64_t)(unit / A.pieces) * A.outer_stride + (int64_t)(unit % A.pieces) * A.piece_stride
                            + begin * A.position_bytes;
     const int64_t bytes = (end - begin) * A.position_bytes, whole = bytes / (int64_t)sizeof(T);
@@ -909,7 +902,8 @@ static void launch_rows_as(const BeamRows& A, hipStream_t stream) {
     const int64_t vectors = A.positions * A.position_bytes / (int64_t)sizeof(T);
     uint32_t splits = (uint32_t)std::min<int64_t>(vectors / 256 + 1, 64);
     splits = std::max<uint32_t>(1, std::min<uint32_t>(splits, 0x7FFFFFFFu / units));
-    hipLaunchKernelGGL((k_beam_reorder_rows<T, MOST>), dim3(units * splits, std::min<uint32_t>(A.groups, 32768), (A.groups + 32767) / 32768), dim3(256), 0, stream, A, splits);
+    hipLaunchKernelGGL((k_beam_reorder_rows<T, MOST>), dim3(units * splits, std::min<uint32_t>(A.groups, 32768), (A.groups + 32767) / 32768), dim3(256), 0, stream,
+                       A.parents, A.begin, A.end, A.beams, splits, A.positions, A);
 }
 
 void launch_beam_reorder_rows(const BeamRows& A, hipStream_t stream) {
