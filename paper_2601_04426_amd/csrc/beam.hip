@@ -749,18 +749,25 @@ __global__ __launch_bounds__(1024) void k_batch_reorder(const int32_t* parents, 
 // A thread has one column of all rows of a group: it loads what every row will hold there and then stores it, so nothing waits for
 // anybody and no second buffer is needed.  Rows that keep their place are neither read (but as parents) nor written.
 // (from: lane k has the row that row k takes; the lane's rows are picked by constants)
-template <class T, int MOST>
+template <class T, int MOST, bool PAST>
 __device__ __forceinline__ void move_column(uint8_t* at, int64_t row_stride, uint32_t from, uint64_t moves) {
     T v[MOST];
 #pragma unroll
     for (int k = 0; k < MOST; ++k)
-        if ((moves >> k) & 1) v[k] = *(Global<const T>)(at + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)from, k) * row_stride);
+        if ((moves >> k) & 1) {
+            const Global<const T> p = (Global<const T>)(at + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)from, k) * row_stride);
+            v[k] = PAST ? __builtin_nontemporal_load(p) : *p;
+        }
 #pragma unroll
     for (int k = 0; k < MOST; ++k)
-        if ((moves >> k) & 1) *(Global<T>)(at + (int64_t)k * row_stride) = v[k];
+        if ((moves >> k) & 1) {
+            const Global<T> p = (Global<T>)(at + (int64_t)k * row_stride);
+            if (PAST) __builtin_nontemporal_store(v[k], p);
+            else *p = v[k];
+        }
 }
 
-template <class T, int MOST>
+template <class T, int MOST, bool PAST>
 __global__ __launch_bounds__(256) void k_beam_reorder_rows(const int32_t* parents, const int32_t* begins, const int32_t* ends, uint32_t K, uint32_t splits, uint32_t positions, BeamRows A) {
     const uint32_t split = blockIdx.x % splits, unit = blockIdx.x / splits, g = blockIdx.y + blockIdx.z * 32768u, lane = threadIdx.x & 63;
     if (g >= A.groups) return;
@@ -775,9 +782,9 @@ __global__ __launch_bounds__(256) void k_beam_reorder_rows(const int32_t* parent
     uint8_t* const piece = A.data + (int64_t)(g * K) * A.row_stride + (int64_t)(unit / A.pieces) * A.outer_stride + (int64_t)(unit % A.pieces) * A.piece_stride
                            + begin * A.position_bytes;
     const int64_t bytes = (end - begin) * A.position_bytes, whole = bytes / (int64_t)sizeof(T);
-    for (int64_t v = (int64_t)split * 256 + threadIdx.x; v < whole; v += (int64_t)splits * 256) move_column<T, MOST>(piece + v * (int64_t)sizeof(T), A.row_stride, from, moves);
+    for (int64_t v = (int64_t)split * 256 + threadIdx.x; v < whole; v += (int64_t)splits * 256) move_column<T, MOST, PAST>(piece + v * (int64_t)sizeof(T), A.row_stride, from, moves);
     const int64_t rest = whole * (int64_t)sizeof(T) + threadIdx.x;   // (less than a vector)
-    if (split == 0 && rest < bytes) move_column<uint8_t, MOST>(piece + rest, A.row_stride, from, moves);
+    if (split == 0 && rest < bytes) move_column<uint8_t, MOST, false>(piece + rest, A.row_stride, from, moves);
 }
 
 // ---- sequences ------------------------------------------------------------------------------------------------------
@@ -896,13 +903,19 @@ void launch_batch_reorder(const BatchDev& D, uint32_t beams, const int32_t* pare
     else hipLaunchKernelGGL(k_batch_reorder<4>, grid, block, 0, stream, parents_dev, D.rows, beams, D, status_dev);
 }
 
+constexpr int64_t ROWS_PAST_BYTES = 256ll << 20;
+constexpr uint32_t ROWS_SPLITS = 16, ROWS_GROUPS = 4096;
+
 template <class T, int MOST>
 static void launch_rows_as(const BeamRows& A, hipStream_t stream) {
     const uint32_t units = A.outer * A.pieces;
-    const int64_t vectors = A.positions * A.position_bytes / (int64_t)sizeof(T);
-    uint32_t splits = (uint32_t)std::min<int64_t>(vectors / 256 + 1, 64);
+    const int64_t piece = A.positions * A.position_bytes, vectors = piece / (int64_t)sizeof(T);
+    const uint64_t all = (uint64_t)units * A.groups, most = std::max<uint64_t>(ROWS_SPLITS, ROWS_GROUPS / all);
+    uint32_t splits = (uint32_t)std::min<uint64_t>((uint64_t)vectors / 256 + 1, most);
     splits = std::max<uint32_t>(1, std::min<uint32_t>(splits, 0x7FFFFFFFu / units));
-    hipLaunchKernelGGL((k_beam_reorder_rows<T, MOST>), dim3(units * splits, std::min<uint32_t>(A.groups, 32768), (A.groups + 32767) / 32768), dim3(256), 0, stream,
+    const bool past = (double)piece * (double)all * A.beams > (double)ROWS_PAST_BYTES;
+    auto* const kernel = past ? k_beam_reorder_rows<T, MOST, true> : k_beam_reorder_rows<T, MOST, false>;
+    hipLaunchKernelGGL(kernel, dim3(units * splits, std::min<uint32_t>(A.groups, 32768), (A.groups + 32767) / 32768), dim3(256), 0, stream,
                        A.parents, A.begin, A.end, A.beams, splits, A.positions, A);
 }
 
