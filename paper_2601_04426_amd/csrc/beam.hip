@@ -241,7 +241,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
 // ---- the best candidates of a group ---------------------------------------------------------------------------------
 // One workgroup per group.  How near a score is to the best is measured in bins whose width grows with the distance (64 to an octave
 // from 2^-6 on).  A count of the pieces' best scores gives the bin that the n-th best of them lies in: at least n candidates lie in it or
-// below, so only pieces, in them blocks, in them tokens that do are looked at, which are few more than n.  16 lanes have a row's pieces.
+// below, so only pieces, in them blocks, in them tokens that do are looked at, which are few more than n as a rule.  Where they are not (fewer
+// pieces than candidates, rows that differ much), blocks, and then tokens, are counted again.  16 lanes have a row's pieces.
 constexpr int kPickThreads = 1024, kPickMostWaves = kPickThreads / 64, kPickBins = 1024, kPickListed = 1024, kPickElems = 2048, kPickHeld = 5;
 
 constexpr uint32_t kRowShift = 26, kRowBits = (1u << kRowShift) - 1;
@@ -579,19 +580,25 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
         for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) count(bin_if(k, ((Global<const float>)(stats + p))[2]));
     } else if (state == ROW_ENDED && part == 0) count(bin_of(top, S.base[k]));
     __syncthreads();
-    uint32_t last_bin = kPickBins - 1;                               // (every wavefront for itself)
-    {
+    // The bin of the n-th best of what was counted (every wavefront for itself), one more: what lies within A.near of it; if fewer were counted, the last.
+    auto bin_of_nth = [&] {
         uint32_t n[16], sum = 0;
         _Pragma("unroll") for (uint32_t i = 0; i < 16; ++i) { n[i] = S.bins[i * 64 + lane]; sum += n[i]; }
         const uint32_t upto = count_upto(sum);
         const unsigned long long reached = __ballot(upto >= N);
-        if (reached != 0) {
-            uint32_t at = upto - sum, b = 0;
-            _Pragma("unroll") for (uint32_t i = 0; i < 16; ++i) { at += n[i]; b += at < N ? 1u : 0u; }
-            // one bin more: what lies within A.near of the n-th best
-            last_bin = (uint32_t)__builtin_amdgcn_readlane((int)(lane * 16 + b + 1), __ffsll((long long)reached) - 1);
-        }
-    }
+        if (reached == 0) return (uint32_t)kPickBins - 1;
+        uint32_t at = upto - sum, b = 0;
+        _Pragma("unroll") for (uint32_t i = 0; i < 16; ++i) { at += n[i]; b += at < N ? 1u : 0u; }
+        return (uint32_t)min(__builtin_amdgcn_readlane((int)(lane * 16 + b + 1), __ffsll((long long)reached) - 1), kPickBins - 1);
+    };
+    auto count_anew = [&] {
+        __syncthreads();
+        for (uint32_t i = tid; i < kPickBins; i += blockDim.x) S.bins[i] = 0;
+        if (tid == 0) S.n_blocks = 0;
+        __syncthreads();
+        if (state == ROW_ENDED && part == 0) count(bin_of(top, S.base[k]));
+    };
+    uint32_t last_bin = bin_of_nth();
     // the pieces that can hold one of the n best, of them the blocks, of them and the ended beams the candidates that can be one
     auto list_piece = [&](uint32_t p) { const uint32_t at = atomicAdd(&S.n_pieces, 1u); if (at < kPickListed) S.pieces[at] = k << kRowShift | p; };
     auto list_candidate = [&](double v, uint64_t at, float x) {
@@ -601,52 +608,79 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
     if (state == ROW_LIVE) {
         _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) if (bin[i] <= last_bin) list_piece(part + i * 16);
         for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) if (bin_if(k, ((Global<const float>)(stats + p))[2]) <= last_bin) list_piece(p);
-    } else if (state == ROW_ENDED && part == 0) list_candidate(S.base[k], place_of(k, -1), 0.f);
+    }
     __syncthreads();
     const uint32_t n_pieces = min(S.n_pieces, (uint32_t)kPickListed);
-    for (uint32_t i0 = tid; i0 < n_pieces * kBeamPieceBlocks; i0 += 4 * blockDim.x) {
-        uint32_t at[4];                                              // (four loads before the first is used)
-        float m[4];
-        _Pragma("unroll") for (int q = 0; q < 4; ++q) {
-            const uint32_t i = i0 + q * blockDim.x;
-            m[q] = NINF;
-            if (i >= n_pieces * kBeamPieceBlocks) continue;
-            const uint32_t piece = S.pieces[i / kBeamPieceBlocks], row_k = piece >> kRowShift, block = (piece & kRowBits) * kBeamPieceBlocks + i % kBeamPieceBlocks;
-            at[q] = row_k << kRowShift | block;
-            m[q] = ((Global<const float>)A.block_max)[(size_t)(g * K + row_k) * pieces * kBeamPieceBlocks + block];
+    auto each_block = [&](auto&& visit) {
+        for (uint32_t i0 = tid; i0 < n_pieces * kBeamPieceBlocks; i0 += 4 * blockDim.x) {
+            uint32_t at[4];                                          // (four loads before the first is used)
+            float m[4];
+            _Pragma("unroll") for (int q = 0; q < 4; ++q) {
+                const uint32_t i = i0 + q * blockDim.x;
+                m[q] = NINF;
+                if (i >= n_pieces * kBeamPieceBlocks) continue;
+                const uint32_t piece = S.pieces[i / kBeamPieceBlocks], row_k = piece >> kRowShift, block = (piece & kRowBits) * kBeamPieceBlocks + i % kBeamPieceBlocks;
+                at[q] = row_k << kRowShift | block;
+                m[q] = ((Global<const float>)A.block_max)[(size_t)(g * K + row_k) * pieces * kBeamPieceBlocks + block];
+            }
+            _Pragma("unroll") for (int q = 0; q < 4; ++q) if (m[q] > NINF) visit(at[q], bin_if(at[q] >> kRowShift, m[q]));
         }
-        _Pragma("unroll") for (int q = 0; q < 4; ++q) {
-            if (!(m[q] > NINF) || bin_if(at[q] >> kRowShift, m[q]) > last_bin) continue;
+    };
+    for (bool counted = last_bin == kPickBins - 1;; counted = true) {
+        if (counted) {
+            count_anew();
+            each_block([&](uint32_t, uint32_t b) { count(b); });
+            __syncthreads();
+            last_bin = min(last_bin, bin_of_nth());
+        }
+        each_block([&](uint32_t at, uint32_t b) {
+            if (b > last_bin) return;
             const uint32_t n = atomicAdd(&S.n_blocks, 1u);
-            if (n < kPickListed) S.blocks[n] = at[q];
-        }
+            if (n < kPickListed) S.blocks[n] = at;
+        });
+        __syncthreads();
+        if (counted || S.n_blocks <= N + N / 2 + 16) break;
     }
     for (uint32_t i = tid; i < kPickElems; i += blockDim.x) S.place[i] = 0;
-    __syncthreads();
     // four lanes have a block, each of them 16 tokens
-    const uint32_t listed = min(S.n_blocks, (uint32_t)kPickListed);
-    const double reach = last_bin < kPickBins - 1 ? top - reach_of(last_bin) : none;
-    for (uint32_t i = tid >> 2; i < listed; i += blockDim.x >> 2) {
-        const uint32_t block = S.blocks[i], row_k = block >> kRowShift, row_r = g * K + row_k;
-        const int t0 = (int)((block & kRowBits) * kBeamBlock + 16 * (tid & 3)) - before_row(static_cast<const E*>(A.logits) + (long long)row_r * A.row_stride);
-        float x[16];
-        const uint32_t ok = load_16<E>(A, row_r, t0, false, x);
-        // a bound in 32 bits first
-        const double least = reach - S.base[row_k];
-        const float bound = (float)least - (__builtin_fabsf((float)least) * 1e-6f + 1e-3f);
-        uint32_t hits = 0;
-        _Pragma("unroll") for (int c = 0; c < 16; ++c) hits |= x[c] >= bound ? 1u << c : 0u;
-        for (hits &= ok; hits != 0; hits &= hits - 1) {
-            const int c = __ffs((int)hits) - 1;
-            float v = x[0];
-            _Pragma("unroll") for (int q = 1; q < 16; ++q) v = c == q ? x[q] : v;
-            if (!(v > NINF)) continue;
-            const double score = score_of(S, row_k, v);
-            if (score > none && bin_of(top, score) <= last_bin) list_candidate(score, place_of(row_k, t0 + c), v);
+    const uint32_t listed_all = S.n_blocks, listed = min(listed_all, (uint32_t)kPickListed);
+    auto each_token = [&](auto&& visit) {
+        const double reach = last_bin < kPickBins - 1 ? top - reach_of(last_bin) : none;
+        for (uint32_t i = tid >> 2; i < listed; i += blockDim.x >> 2) {
+            const uint32_t block = S.blocks[i], row_k = block >> kRowShift, row_r = g * K + row_k;
+            const int t0 = (int)((block & kRowBits) * kBeamBlock + 16 * (tid & 3)) - before_row(static_cast<const E*>(A.logits) + (long long)row_r * A.row_stride);
+            float x[16];
+            const uint32_t ok = load_16<E>(A, row_r, t0, false, x);
+            // a bound in 32 bits first
+            const double least = reach - S.base[row_k];
+            const float bound = (float)least - (__builtin_fabsf((float)least) * 1e-6f + 1e-3f);
+            uint32_t hits = 0;
+            _Pragma("unroll") for (int c = 0; c < 16; ++c) hits |= x[c] >= bound ? 1u << c : 0u;
+            for (hits &= ok; hits != 0; hits &= hits - 1) {
+                const int c = __ffs((int)hits) - 1;
+                float v = x[0];
+                _Pragma("unroll") for (int q = 1; q < 16; ++q) v = c == q ? x[q] : v;
+                if (!(v > NINF)) continue;
+                const double score = score_of(S, row_k, v);
+                if (score > none) visit(score, row_k, t0 + c, v);
+            }
         }
+    };
+    for (bool counted = last_bin == kPickBins - 1 && listed > 4;; counted = true) {
+        if (counted) {
+            count_anew();
+            each_token([&](double score, uint32_t, int, float) { count(bin_of(top, score)); });
+            __syncthreads();
+            last_bin = min(last_bin, bin_of_nth());
+            if (tid == 0) S.n_elems = 0;
+            __syncthreads();
+        }
+        if (state == ROW_ENDED && part == 0) list_candidate(S.base[k], place_of(k, -1), 0.f);
+        each_token([&](double score, uint32_t row_k, int t, float v) { if (bin_of(top, score) <= last_bin) list_candidate(score, place_of(row_k, t), v); });
+        __syncthreads();
+        if (counted || S.n_elems <= 2 * N + 64) break;
     }
-    __syncthreads();
-    if (S.n_pieces > kPickListed || S.n_blocks > kPickListed || S.n_elems > kPickElems) { pick_one_by_one<E>(A, S, g); return; }
+    if (S.n_pieces > kPickListed || listed_all > kPickListed || S.n_elems > kPickElems) { pick_one_by_one<E>(A, S, g); return; }
     const uint32_t R = S.n_elems;
     for (;;) {
         // A candidate's place is the number of candidates before it: a wavefront compares 64 candidates with its part of all.
