@@ -350,7 +350,7 @@ int32_t xg2_batch_reorder(xg2_batch*, int32_t beams, const int32_t* parents_dev,
  * layers and pieces = heads, [layers, rows, positions, heads, width] outer = layers, pieces = 1 and position_bytes of all heads.
  * begin_dev, end_dev (device, G int32 each, may be NULL: 0 and positions): only positions begin[g] <= t < end[g] of group g's
  * rows are touched (its beams have the prompt in common); values outside 0 .. positions count as these.  Pieces must not
- * overlap.  parents_dev: device, G * K int32, each in its row's group; rows with -1, or any row outside the group, stay.    */
+ * overlap, and there are at most 2^23 of them in a row.  parents_dev: device, G * K int32, each in its row's group; rows with -1, or any row outside the group, stay.    */
 int32_t xg2_beam_reorder_rows(void* data_dev, int32_t groups, int32_t beams, const int32_t* parents_dev, int64_t row_stride,
                               int32_t outer, int64_t outer_stride, int32_t pieces, int64_t piece_stride, int32_t positions,
                               int64_t position_bytes, const int32_t* begin_dev, const int32_t* end_dev, void* hip_stream);

@@ -103,7 +103,7 @@ int32_t xg2_beam_reorder_rows(void* data_dev, int32_t groups, int32_t beams, con
         const char* const me = "xg2_beam_reorder_rows";
         if (groups < 0 || beams < 1 || (uint32_t)beams > kBeamsMost || outer < 0 || pieces < 0 || positions < 0 || position_bytes < 0) return bad(me, "bad argument");
         if ((int64_t)groups * beams > (int64_t)kBeamRowsMost) return bad(me, "more than 2^20 rows");
-        if ((int64_t)outer * pieces > INT32_MAX) return bad(me, "more than 2^31 - 1 pieces a row");
+        if ((int64_t)outer * pieces > (int64_t)kBeamPiecesMost) return bad(me, "more than 2^23 pieces a row");
         if (groups == 0 || outer == 0 || pieces == 0 || positions == 0 || position_bytes == 0 || beams == 1) return XG2_OK;
         if (!data_dev || !parents_dev) return bad(me, "null buffer");
         if (!aligned(parents_dev, 4) || !aligned(begin_dev, 4) || !aligned(end_dev, 4)) return bad(me, "buffer of words off a multiple of 4 bytes");

@@ -834,7 +834,10 @@ __global__ __launch_bounds__(kTraceThreads) void k_beam_backtrace(BeamTrace A, u
     constexpr uint32_t NONE = 255;
     __shared__ uint8_t maps[2][kTraceThreads];                       // [segment * WIDTH + beam behind it]: the beam before it
     __shared__ int32_t last[WIDTH];                                  // steps up to and with a sequence's last token
-    const uint32_t g = blockIdx.x, K = A.beams, lane = threadIdx.x & 63, k = lane % WIDTH, base = lane - k, first = g * K, s = threadIdx.x / WIDTH;
+    // (groups that lie side by side share cache lines of a step: they go to one die, which every eighth workgroup does)
+    const uint32_t g = blockIdx.x % 8 * ((A.groups + 7) / 8) + blockIdx.x / 8;
+    if (g >= A.groups) return;
+    const uint32_t K = A.beams, lane = threadIdx.x & 63, k = lane % WIDTH, base = lane - k, first = g * K, s = threadIdx.x / WIDTH;
     const uint32_t from = s * length, to = s < segments ? min(from + length, A.steps) : from;
     const bool mine = k < K;
     const uint32_t row = first + (mine ? k : 0);
@@ -946,7 +949,7 @@ static void launch_rows_as(const BeamRows& A, hipStream_t stream) {
     const int64_t piece = A.positions * A.position_bytes, vectors = piece / (int64_t)sizeof(T);
     const uint64_t all = (uint64_t)units * A.groups, most = std::max<uint64_t>(ROWS_SPLITS, ROWS_GROUPS / all);
     uint32_t splits = (uint32_t)std::min<uint64_t>((uint64_t)vectors / 256 + 1, most);
-    splits = std::max<uint32_t>(1, std::min<uint32_t>(splits, 0x7FFFFFFFu / units));
+    splits = std::max<uint32_t>(1, std::min<uint32_t>(splits, (1u << 23) / units));            // (a grid has less than 2^32 threads)
     const bool past = (double)piece * (double)all * A.beams > (double)ROWS_PAST_BYTES;
     auto* const kernel = past ? k_beam_reorder_rows<T, MOST, true> : k_beam_reorder_rows<T, MOST, false>;
     hipLaunchKernelGGL(kernel, dim3(units * splits, std::min<uint32_t>(A.groups, 32768), (A.groups + 32767) / 32768), dim3(256), 0, stream,
@@ -968,7 +971,7 @@ static void launch_backtrace_as(const BeamTrace& A, hipStream_t stream) {
     constexpr uint32_t most = kTraceThreads / WIDTH;
     const uint32_t length = std::max<uint32_t>(8, (A.steps + most - 1) / most), segments = (A.steps + length - 1) / length;
     const uint32_t threads = std::max<uint32_t>(64, (segments * WIDTH + 63) / 64 * 64);
-    hipLaunchKernelGGL(k_beam_backtrace<WIDTH>, dim3(A.groups), dim3(threads), 0, stream, A, segments, length);
+    hipLaunchKernelGGL(k_beam_backtrace<WIDTH>, dim3((A.groups + 7) / 8 * 8), dim3(threads), 0, stream, A, segments, length);
 }
 
 void launch_beam_backtrace(const BeamTrace& A, hipStream_t stream) {

@@ -33,15 +33,16 @@ struct BeamSelect {
     double near;                                            // scores of different rows closer than this are compared with sums in 64 bits
 };
 // How far the difference of two rows' scores may be off by their sums in 32 bits: twice what one sum may be off, relative to its value.
-// A term exp2(t), t = x log2(e) - c, is off by one unit of exp2 (2^-23) and by the rounding of t, |t| 2^-24 ln 2 = (top - x) 2^-24,
-// whose mean over the probabilities is at most ln V; between a term and its piece's sum lie 11 additions of 2^-24 each.  (Pieces are
-// joined in 64 bits.)
-inline double beam_near(int32_t V) { return (std::log((double)(V < 2 ? 2 : V)) + 2 + 11) / (1 << 23); }
+// A term 2^t, t = x log2(e) - c, is off by one unit of the exponential (2^-23), by the rounding of t (|t| 2^-24 ln 2 = (top - x) 2^-24)
+// and by that of log2(e) to 32 bits, which is made good for the largest x and leaves (top - x) 0.23 2^-24; the mean of top - x over the
+// probabilities is at most ln V.  Between a term and its piece's sum lie 11 additions of 2^-24 each.  (Pieces are joined in 64 bits.)
+inline double beam_near(int32_t V) { return (1.23 * std::log((double)(V < 2 ? 2 : V)) + 2 + 11) / (1 << 23); }
 void launch_beam_select(const BeamSelect& A, hipStream_t stream);
 
 // ---- reordering -----------------------------------------------------------------------------------------------------
 void launch_batch_reorder(const BatchDev& D, uint32_t beams, const int32_t* parents_dev, int32_t* status_dev, hipStream_t stream);
 
+constexpr uint32_t kBeamPiecesMost = 1u << 23;              // pieces of a row of a buffer: a workgroup of 256 threads each at the least
 struct BeamRows {
     uint8_t* data; const int32_t* parents;
     const int32_t* begin; const int32_t* end;               // [groups] positions, or null: all

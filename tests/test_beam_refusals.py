@@ -63,7 +63,7 @@ def test_select_workspace(xg):
 
 @pytest.mark.parametrize("kw", [
     dict(groups=-1), dict(beams=0), dict(beams=65), dict(groups=1 << 20, beams=2), dict(outer=-1), dict(pieces=-1), dict(positions=-1), dict(position_bytes=-1),
-    dict(outer=1 << 20, pieces=1 << 20), dict(data_ptr=0), dict(parents_ptr=0), dict(parents_ptr=P + 2), dict(begin_ptr=P + 1), dict(end_ptr=P + 2),
+    dict(outer=1 << 20, pieces=1 << 20), dict(outer=1, pieces=(1 << 23) + 1), dict(data_ptr=0), dict(parents_ptr=0), dict(parents_ptr=P + 2), dict(begin_ptr=P + 1), dict(end_ptr=P + 2),
     dict(row_stride=64 * 16 - 1), dict(row_stride=-8192), dict(piece_stride=1000), dict(outer_stride=0), dict(positions=1 << 30, position_bytes=1 << 40)])
 def test_rows_refuse(xg, kw):
     assert "xg2_beam_reorder_rows" in refused(xg, rows, **kw)
