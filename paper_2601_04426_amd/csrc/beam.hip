@@ -85,7 +85,7 @@ constexpr double LN2 = 0.693147180559945309417232;
 typedef uint32_t Vec4 __attribute__((ext_vector_type(4)));
 // vectors at any byte: the device takes them
 typedef uint32_t Wide4 __attribute__((ext_vector_type(4), aligned(1)));
-typedef uint32_t Wide2 __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t Wide1 __attribute__((aligned(1)));
 template <class E> struct Elem;
 template <> struct Elem<float> {
     static constexpr int EPV = 4;
@@ -782,26 +782,38 @@ __global__ __launch_bounds__(1024) void k_batch_reorder(const int32_t* parents, 
 // ---- rows of a buffer -----------------------------------------------------------------------------------------------
 // A thread has one column of all rows of a group: it loads what every row will hold there and then stores it, so nothing waits for
 // anybody and no second buffer is needed.  Rows that keep their place are neither read (but as parents) nor written.
-// (from: lane k has the row that row k takes; the lane's rows are picked by constants)
-template <class T, int MOST, bool PAST>
-__device__ __forceinline__ void move_column(uint8_t* at, int64_t row_stride, uint32_t from, uint64_t moves) {
-    T v[MOST];
+// TOGETHER columns of a thread, `apart` bytes from one to the next, of which `n` exist.  (from: lane k has the row that row k takes; the
+// lane's rows are picked by constants.  What a row's number makes of its stride is worked out anew where it is used: kept for all rows
+// it would not fit the scalar registers.)
+template <class T, int MOST, int TOGETHER, bool PAST>
+__device__ __forceinline__ void move_columns(uint8_t* at, int64_t apart, int n, int64_t row_stride, uint32_t from, uint64_t moves) {
+    T v[TOGETHER][MOST];
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+s"(row_stride));
+#endif
 #pragma unroll
-    for (int k = 0; k < MOST; ++k)
-        if ((moves >> k) & 1) {
-            const Global<const T> p = (Global<const T>)(at + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)from, k) * row_stride);
-            v[k] = PAST ? __builtin_nontemporal_load(p) : *p;
-        }
+    for (int k = 0; k < MOST; ++k) {
+        if (!((moves >> k) & 1)) continue;
+        const uint8_t* const row = at + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)from, k) * row_stride;
+        _Pragma("unroll") for (int j = 0; j < TOGETHER; ++j)
+            if (j < n) v[j][k] = PAST ? __builtin_nontemporal_load((Global<const T>)(row + j * apart)) : *(Global<const T>)(row + j * apart);
+    }
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+s"(row_stride));
+#endif
 #pragma unroll
-    for (int k = 0; k < MOST; ++k)
-        if ((moves >> k) & 1) {
-            const Global<T> p = (Global<T>)(at + (int64_t)k * row_stride);
-            if (PAST) __builtin_nontemporal_store(v[k], p);
-            else *p = v[k];
+    for (int k = 0; k < MOST; ++k) {
+        if (!((moves >> k) & 1)) continue;
+        uint8_t* const row = at + (int64_t)k * row_stride;
+        _Pragma("unroll") for (int j = 0; j < TOGETHER; ++j) {
+            if (j >= n) continue;
+            if (PAST) __builtin_nontemporal_store(v[j][k], (Global<T>)(row + j * apart));
+            else *(Global<T>)(row + j * apart) = v[j][k];
         }
+    }
 }
 
-template <class T, int MOST, bool PAST>
+template <class T, int MOST, int TOGETHER, bool PAST>
 __global__ __launch_bounds__(256) void k_beam_reorder_rows(const int32_t* parents, const int32_t* begins, const int32_t* ends, uint32_t K, uint32_t splits, uint32_t positions, BeamRows A) {
     const uint32_t split = blockIdx.x % splits, unit = blockIdx.x / splits, g = blockIdx.y + blockIdx.z * 32768u, lane = threadIdx.x & 63;
     if (g >= A.groups) return;
@@ -815,10 +827,14 @@ __global__ __launch_bounds__(256) void k_beam_reorder_rows(const int32_t* parent
     if (moves == 0) return;
     uint8_t* const piece = A.data + (int64_t)(g * K) * A.row_stride + (int64_t)(unit / A.pieces) * A.outer_stride + (int64_t)(unit % A.pieces) * A.piece_stride
                            + begin * A.position_bytes;
-    const int64_t bytes = (end - begin) * A.position_bytes, whole = bytes / (int64_t)sizeof(T);
-    for (int64_t v = (int64_t)split * 256 + threadIdx.x; v < whole; v += (int64_t)splits * 256) move_column<T, MOST, PAST>(piece + v * (int64_t)sizeof(T), A.row_stride, from, moves);
-    const int64_t rest = whole * (int64_t)sizeof(T) + threadIdx.x;   // (less than a vector)
-    if (split == 0 && rest < bytes) move_column<uint8_t, MOST, false>(piece + rest, A.row_stride, from, moves);
+    constexpr int64_t SIZE = sizeof(T);
+    const int64_t bytes = (end - begin) * A.position_bytes, whole = bytes / SIZE;
+    for (int64_t v = (int64_t)split * 256 * TOGETHER + threadIdx.x; v < whole; v += (int64_t)splits * 256 * TOGETHER) {
+        const int64_t left = (whole - v + 255) / 256;
+        move_columns<T, MOST, TOGETHER, PAST>(piece + v * SIZE, 256 * SIZE, left < TOGETHER ? (int)left : TOGETHER, A.row_stride, from, moves);
+    }
+    const int64_t rest = whole * SIZE + threadIdx.x;                 // (less than a vector)
+    if (split == 0 && rest < bytes) move_columns<uint8_t, MOST, 1, false>(piece + rest, 0, 1, A.row_stride, from, moves);
 }
 
 // ---- sequences ------------------------------------------------------------------------------------------------------
@@ -940,29 +956,38 @@ void launch_batch_reorder(const BatchDev& D, uint32_t beams, const int32_t* pare
     else hipLaunchKernelGGL(k_batch_reorder<4>, grid, block, 0, stream, parents_dev, D.rows, beams, D, status_dev);
 }
 
+// Buffers beyond the last-level cache (256 MB) are moved past it: what is moved is not there when attention reads the whole buffer, moved or
+// not.  Through the caches / past them, us, 8 beams, 64 pieces of 32 kB a row: 256 MB (below the line) 53.4 / 48.5, 320 MB 66.6 / 60.5,
+// 512 MB 98.9 / 90.7; below the line what is left in the cache is worth more to the next reader.
+// A piece is cut into at most 16 parts where there are many, or so many that there are 4,096 workgroups: a part beyond a group's window
+// costs a workgroup that finds nothing to do (19 groups, 6 pieces of 313 kB, windows of a quarter, at most 64 / 16 / 8 parts: 16.0 / 13.1 / 13.4
+// us; one piece of 100 MB a row, 16 / 64 / 4,096 parts: 806 / 219 / 46).
 constexpr int64_t ROWS_PAST_BYTES = 256ll << 20;
 constexpr uint32_t ROWS_SPLITS = 16, ROWS_GROUPS = 4096;
 
-template <class T, int MOST>
+template <class T, int MOST, int TOGETHER>
 static void launch_rows_as(const BeamRows& A, hipStream_t stream) {
     const uint32_t units = A.outer * A.pieces;
     const int64_t piece = A.positions * A.position_bytes, vectors = piece / (int64_t)sizeof(T);
     const uint64_t all = (uint64_t)units * A.groups, most = std::max<uint64_t>(ROWS_SPLITS, ROWS_GROUPS / all);
-    uint32_t splits = (uint32_t)std::min<uint64_t>((uint64_t)vectors / 256 + 1, most);
+    uint32_t splits = (uint32_t)std::min<uint64_t>((uint64_t)vectors / (256 * TOGETHER) + 1, most);
     splits = std::max<uint32_t>(1, std::min<uint32_t>(splits, (1u << 23) / units));            // (a grid has less than 2^32 threads)
     const bool past = (double)piece * (double)all * A.beams > (double)ROWS_PAST_BYTES;
-    auto* const kernel = past ? k_beam_reorder_rows<T, MOST, true> : k_beam_reorder_rows<T, MOST, false>;
+    auto* const kernel = past ? k_beam_reorder_rows<T, MOST, TOGETHER, true> : k_beam_reorder_rows<T, MOST, TOGETHER, false>;
     hipLaunchKernelGGL(kernel, dim3(units * splits, std::min<uint32_t>(A.groups, 32768), (A.groups + 32767) / 32768), dim3(256), 0, stream,
                        A.parents, A.begin, A.end, A.beams, splits, A.positions, A);
 }
 
+// What a thread holds of each row, and how many columns of it.  TB/s over 537 MB (rows of 256 positions of 128 bytes, moved bytes counted
+// once read and once written), 2 / 4 / 8 / 16 / 32 / 64 beams: 16 bytes, one column 3.3 / 5.4 / 5.2 / 4.8 / 3.9 / -, two columns 4.8 / 5.1 / 5.0
+// / - / - / - (their registers cost wavefronts), 8 bytes - / - / - / - / 3.1 / 2.2, 4 bytes - / - / - / - / 4.2 / 3.3.
 void launch_beam_reorder_rows(const BeamRows& A, hipStream_t stream) {
-    // what a thread holds is a vector a row
-    if (A.beams <= 4) launch_rows_as<Wide4, 4>(A, stream);
-    else if (A.beams <= 8) launch_rows_as<Wide4, 8>(A, stream);
-    else if (A.beams <= 16) launch_rows_as<Wide4, 16>(A, stream);
-    else if (A.beams <= 32) launch_rows_as<Wide4, 32>(A, stream);
-    else launch_rows_as<Wide2, 64>(A, stream);
+    if (A.beams <= 2) launch_rows_as<Wide4, 2, 2>(A, stream);
+    else if (A.beams <= 4) launch_rows_as<Wide4, 4, 1>(A, stream);
+    else if (A.beams <= 8) launch_rows_as<Wide4, 8, 1>(A, stream);
+    else if (A.beams <= 16) launch_rows_as<Wide4, 16, 1>(A, stream);
+    else if (A.beams <= 32) launch_rows_as<Wide1, 32, 1>(A, stream);
+    else launch_rows_as<Wide1, 64, 1>(A, stream);
 }
 
 template <int WIDTH>
