@@ -525,8 +525,9 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
         }
         for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) look(stats[p]);
         m = largest_of_16(m);
-        // a NaN or an infinity among what counts, or magnitudes that the sum's exponents cannot take: from the logits again
-        odd |= !(m < 1e6f) || (m > NINF && m < -1e6f);
+        // a NaN or an infinity among what counts, or magnitudes that the sum's exponents cannot take or that leave a score no places behind
+        // the point: from the logits again
+        odd |= !(m < 1e6f) || (m > NINF && m < -1e6f) || !(s < 1e6f && s > -1e6f);
         repair = ((__ballot(odd) >> (lane & 48)) & 0xFFFF) != 0;
         // A piece's sum is of 2^(x * LOG2E - c), c = the rounded product of its maximum and LOG2E; LOG2E itself is off by `off`.
         const double off = (double)LOG2E - 1.4426950408889634073599, mc = (double)__fmul_rn(m, LOG2E) - (double)m * off;
@@ -691,7 +692,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
             uint32_t n = 0;
             for (uint32_t q = wave; q < sixteenths; q += waves) {
                 const uint32_t to = min(q * 16 + 16, R);
-                _Pragma("unroll 4") for (uint32_t j = q * 16; j < to; ++j) { const Candidate o = S.found[j]; n += before(o, c) ? 1u : 0u; }
+                _Pragma("unroll 8") for (uint32_t j = q * 16; j < to; ++j) { const Candidate o = S.found[j]; n += before(o, c) ? 1u : 0u; }
             }
             if (i < R && n != 0) atomicAdd(&S.place[i], n);
         }

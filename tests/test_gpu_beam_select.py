@@ -123,6 +123,35 @@ def test_groups_and_candidates(xg, dtype, G, K, n):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K,V,n", [(1, 60, 128), (1, 500, 16), (1, 5000, 128), (2, 129, 128), (4, 2000, 8), (4, 300, 100), (8, 8000, 16), (32, 2000, 32), (64, 100, 128), (3, 70000, 128)])
+def test_rows_that_differ_and_few_pieces(xg, dtype, K, V, n):
+    """Rows from nearly everything allowed to a handful, and fewer pieces or blocks of the vocabulary than candidates wanted."""
+    rng = np.random.default_rng(K * 1000 + V)
+    G = 3
+    x, allowed, scores, finished = _inputs(rng, G, K, V, "mixed")
+    for over_all in (False, True):
+        Call(xg, x, allowed, scores, finished, G, K, n, over_all, dtype).check(over_all)
+    x[::2] -= 6                                                      # every other beam is far behind in all it has
+    Call(xg, x, None, scores, finished, G, K, n, False, dtype).check("behind")
+
+
+def test_large_magnitudes(xg):
+    """Logits and scores whose exponentials or sums a row's first pass cannot take."""
+    rng = np.random.default_rng(10)
+    K, V = 6, 5000
+    x = (rng.standard_normal((K, V)) * 2).astype(np.float32)
+    x[1] *= 1e5
+    x[2] = x[2] * 1e30
+    x[3] += 3e6
+    x[4] -= 2e9
+    x[5, 10:] -= 1e9
+    for scores in (np.full(K, -1.0), np.array([-1.0, -2e5, -3e30, -4e6, 5e6, -6.0]), np.array([2e15, 2e15, 2e15, 1e30, 1e30, -1e30])):
+        for dtype in ("f32", "bf16"):
+            Call(xg, x, None, scores, None, 1, K, 40, False, dtype).check(scores)
+            Call(xg, x, rng.random((K, V)) < 0.5, scores, None, 2, 3, 40, True, dtype).check(scores)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_logits_that_are_alike(xg, dtype):
     """Ties go to the lowest row, then to the lowest token: all logits the same, a handful of values, the same rows again."""
     rng = np.random.default_rng(5)
