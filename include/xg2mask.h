@@ -327,7 +327,7 @@ int32_t xg2_apply_token_bitmask(void* logits_dev, int32_t dtype, int32_t B, int3
  * +infinity counts, the tokens that have it share the probability evenly and the others have none.
  * Out, [G, n_out] each, best first: scores, parents (rows), tokens, and (may be NULL) whether the continuation has ended:
  * 1 if its parent had or its token is eos_id.  Where a group has fewer candidates the rest is -infinity, -1, -1, 1.
- * n_out is between 1 and 128, V at most 2^30.  No output may overlap an input.  workspace_dev: device, 16-byte aligned, at
+ * n_out is between 1 and 128, V at most 2^24.  No output may overlap an input.  workspace_dev: device, 16-byte aligned, at
  * least as many bytes as xg2_beam_select_workspace says, which later calls may use again in stream order.                  */
 #define XG2_OVER_ALLOWED 0
 #define XG2_OVER_ALL     1

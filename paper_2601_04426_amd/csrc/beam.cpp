@@ -31,7 +31,7 @@ const char* bad_shape(int32_t dtype, int32_t groups, int32_t beams, int32_t V, i
     if (dtype != XG2_F32 && dtype != XG2_BF16) return "unknown dtype";
     if (groups < 0 || beams < 1 || (uint32_t)beams > kBeamsMost) return "between 1 and 64 beams a group";
     if ((int64_t)groups * beams > (int64_t)kBeamRowsMost) return "more than 2^20 rows";
-    if (V < 1 || V > kBeamVocabMost) return "between 1 and 2^30 tokens";
+    if (V < 1 || V > kBeamVocabMost) return "between 1 and 2^24 tokens";
     if (n_out < 1 || (uint32_t)n_out > kBeamOutMost) return "between 1 and 128 candidates a group";
     return nullptr;
 }

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
     const uint32_t r = first_row + blockIdx.y, lane = threadIdx.x & 63, piece = blockIdx.x * (blockDim.x >> 6) + uniform(threadIdx.x >> 6);
     if (piece >= pieces) return;
     const E* const row = static_cast<const E*>(logits) + (long long)r * row_stride;
-    const int e0 = (int)piece * kBeamPiece - before_row(row);             // (V is at most 2^30)
+    const int e0 = (int)piece * kBeamPiece - before_row(row);             
     const bool inner = e0 >= 0 && e0 + kBeamPiece <= V;
     // this lane's 32 tokens from e0 + 32 * lane on: which are in the row, and which of them are allowed
     const int first = e0 + 32 * (int)lane;
@@ -310,7 +310,8 @@ __device__ __forceinline__ uint32_t count_upto(uint32_t v) {
 }
 
 __device__ __forceinline__ uint32_t bin_of(double top, double score) {
-    const float d = (float)(top - score) + 0.015625f;                // (monotone: each step rounds one way for all)
+    // (monotone: each step rounds one way for all; logits of 1e30 leave a score nothing of its beam's, and it can lie above the best)
+    const float d = fmaxf((float)(top - score), 0.f) + 0.015625f;
     const uint32_t b = (__float_as_uint(d) >> 17) - (__float_as_uint(0.015625f) >> 17);
     return b < kPickBins - 1 ? b : kPickBins - 1;
 }
@@ -494,22 +495,38 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
     __shared__ PickShared S;
     const uint32_t g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x >> 6;
     constexpr double none = -(double)__builtin_inff();
-    // 16 lanes of a row: the row's sum
+    // 16 lanes have a row.  No score of a row is above its beam's (a logarithm of a probability is at most zero): the best of the beams' is
+    // what distances are taken from, and is known before the sums are.
     const uint32_t k = tid >> 4, part = tid & 15, r = g * K + k;
     const Global<const Vec4> stats = (Global<const Vec4>)(all_stats + (size_t)r * pieces);
     const bool mine = k < K;
     float s = NINF, best[kPickHeld];
     Vec4 held[kPickHeld];
-    bool ended = false;
+    int32_t ended = 0;
     if (mine) {
-        _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) held[i] = stats[min(part + i * 16, pieces - 1)];
         s = ((Global<const float>)scores)[r];
-        if (finished) ended = ((Global<const int32_t>)finished)[r] != 0;
+        if (finished) ended = ((Global<const int32_t>)finished)[r];
+        _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) held[i] = stats[min(part + i * 16, pieces - 1)];
     }
     for (uint32_t i = tid; i < kPickBins; i += blockDim.x) S.bins[i] = 0;
     if (tid == 0) S.n_pieces = S.n_blocks = S.n_elems = 0;
-    uint32_t state = !(s > NINF && s < -NINF) ? ROW_NONE : ended ? ROW_ENDED : ROW_LIVE, repair = 0;
-    double base = s, top = none;                                     // top: no score is above it
+    uint32_t state = !(s > NINF && s < -NINF) ? ROW_NONE : ended != 0 ? ROW_ENDED : ROW_LIVE, repair = 0;
+    {
+        float m = state == ROW_NONE ? NINF : s;
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        if (lane == 0) S.wave_top[wave] = m;
+    }
+    __syncthreads();
+    double top = none, base = s;
+    for (uint32_t w = 0; w < waves; ++w) top = S.wave_top[w] > top ? S.wave_top[w] : top;
+    // how many pieces (and ended beams) have their best score in each bin
+    uint32_t bin[kPickHeld];
+    auto bin_if = [&](uint32_t row, float m) {
+        const double v = score_of(S, row, m);
+        return m > NINF && v > none ? bin_of(top, v) : (uint32_t)kPickBins;
+    };
+    auto count = [&](uint32_t b) { if (b < kPickBins) atomicAdd(&S.bins[bin_at(b)], 1u); };
     if (state == ROW_LIVE) {
         float m = NINF;
         bool odd = false;
@@ -540,47 +557,32 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
         _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) if (i * 16u < pieces) add(held[i]);     // (the same in all lanes)
         for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) add(stats[p]);
         sum = sum_of_16(sum);
-        if (m == NINF) { if (!repair) state = ROW_NONE; }
-        else {
-            base -= log_of(sum) + mc * LN2;
-            top = base + m;
+        if (!repair) {
+            if (m == NINF) state = ROW_NONE;
+            else base -= log_of(sum) + mc * LN2;
+            _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) {
+                bin[i] = best[i] > NINF ? bin_of(top, base + best[i]) : (uint32_t)kPickBins;
+                count(bin[i]);
+            }
+            for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) {
+                const float o = ((Global<const float>)(stats + p))[2];
+                if (o > NINF) count(bin_of(top, base + o));
+            }
         }
-    } else if (state == ROW_ENDED) top = base;
+    } else if (state == ROW_ENDED && part == 0) count(bin_of(top, base));
     if (mine && part == 0) { S.state[k] = state; S.base[k] = base; S.infinite[k] = 0; S.exact[k] = state != ROW_LIVE; S.repair[k] = repair; }
-    {
-        const double a = __shfl_xor(top, 16), ab = top > a ? top : a, c = __shfl_xor(ab, 32);
-        top = ab > c ? ab : c;
-    }
-    if (lane == 0) S.wave_top[wave] = top;
     if (__syncthreads_or((int)repair)) {
         for (uint32_t q = 0; q < K; ++q) if (S.repair[q]) repair_row<E>(A, S, g, q, true);
-        top = none;
-        if (mine) {
-            state = S.state[k];
-            float m = NINF;
-            if (state == ROW_LIVE) {
-                _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) { best[i] = part + i * 16 < pieces ? ((Global<const float>)(stats + part + i * 16))[2] : NINF; m = best[i] > m ? best[i] : m; }
-                for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) { const float o = ((Global<const float>)(stats + p))[2]; m = o > m ? o : m; }
-                top = m > NINF ? score_of(S, k, m) : none;           // (no logit of a row is above its largest)
-            } else if (state == ROW_ENDED) top = S.base[k];
+        if (repair) state = S.state[k];
+        if (repair && state == ROW_LIVE) {
+            _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) {
+                bin[i] = part + i * 16 < pieces ? bin_if(k, ((Global<const float>)(stats + part + i * 16))[2]) : (uint32_t)kPickBins;
+                count(bin[i]);
+            }
+            for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) count(bin_if(k, ((Global<const float>)(stats + p))[2]));
         }
-        for (int d = 1; d < 64; d *= 2) { const double o = __shfl_xor(top, d); top = o > top ? o : top; }
-        if (lane == 0) S.wave_top[wave] = top;
         __syncthreads();
     }
-    for (uint32_t w = 0; w < waves; ++w) top = S.wave_top[w] > top ? S.wave_top[w] : top;
-    // how many pieces (and ended beams) have their best score in each bin
-    uint32_t bin[kPickHeld];
-    auto bin_if = [&](uint32_t row, float m) {
-        const double v = score_of(S, row, m);
-        return m > NINF && v > none ? bin_of(top, v) : (uint32_t)kPickBins;
-    };
-    auto count = [&](uint32_t b) { if (b < kPickBins) atomicAdd(&S.bins[bin_at(b)], 1u); };
-    if (state == ROW_LIVE) {
-        _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) { bin[i] = bin_if(k, best[i]); count(bin[i]); }
-        for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) count(bin_if(k, ((Global<const float>)(stats + p))[2]));
-    } else if (state == ROW_ENDED && part == 0) count(bin_of(top, S.base[k]));
-    __syncthreads();
     // The bin of the n-th best of what was counted (every wavefront for itself), one more: what lies within A.near of it; if fewer were counted, the last.
     auto bin_of_nth = [&] {
         uint32_t n[16], sum = 0;

@@ -11,7 +11,7 @@ namespace xg2 {
 
 // ---- selection ------------------------------------------------------------------------------------------------------
 constexpr uint32_t kBeamsMost = 64, kBeamOutMost = 128;     // beams of a group; candidates chosen for one
-constexpr int32_t kBeamVocabMost = 1 << 30;
+constexpr int32_t kBeamVocabMost = 1 << 24;
 constexpr uint32_t kBeamRowsMost = 1u << 20;
 constexpr int kBeamPiece = 2048, kBeamBlock = 64;           // tokens that a wavefront takes; tokens that share a maximum
 constexpr int kBeamPieceBlocks = kBeamPiece / kBeamBlock;

@@ -41,7 +41,7 @@ def refused(xg, call, code=EINVAL, **kw):
 
 
 @pytest.mark.parametrize("kw", [
-    dict(dtype=2), dict(dtype=-1), dict(groups=-1), dict(beams=0), dict(beams=65), dict(groups=1 << 20, beams=2), dict(V=0), dict(V=-5), dict(V=(1 << 30) + 1, row_stride_elems=1 << 31),
+    dict(dtype=2), dict(dtype=-1), dict(groups=-1), dict(beams=0), dict(beams=65), dict(groups=1 << 20, beams=2), dict(V=0), dict(V=-5), dict(V=(1 << 24) + 1, row_stride_elems=1 << 31),
     dict(n_out=0), dict(n_out=129), dict(over=2), dict(over=-1), dict(row_stride_elems=999), dict(bm_row_stride_words=31), dict(logits_ptr=0), dict(scores_ptr=0),
     dict(out_scores_ptr=0), dict(out_parents_ptr=0), dict(out_tokens_ptr=0), dict(workspace_ptr=0), dict(workspace_ptr=P + 8), dict(workspace_bytes=100), dict(logits_ptr=P + 2),
     dict(scores_ptr=P + 1), dict(out_tokens_ptr=P + 2), dict(finished_ptr=P + 3), dict(out_finished_ptr=P + 2), dict(bitmask_ptr=P + 2)])
@@ -53,7 +53,7 @@ def test_select_workspace(xg):
     n = xg.beam_select_workspace(xg.XG2_BF16, 2, 4, 1000, 4)
     refused(xg, select, dtype=xg.XG2_BF16, workspace_bytes=n - 1)
     assert xg.beam_select_workspace(xg.XG2_F32, 0, 4, 1000, 4) == 0
-    assert xg.beam_select_workspace(xg.XG2_F32, 1, 1, 1 << 30, 128) > 0
+    assert xg.beam_select_workspace(xg.XG2_F32, 1, 1, 1 << 24, 128) > 0
     for bad in ((2, 1, 1, 10, 1), (0, -1, 1, 10, 1), (0, 1, 65, 10, 1), (0, 1, 1, 0, 1), (0, 1, 1, 10, 0), (0, 1, 1, 10, 129)):
         with pytest.raises(xg.Xg2Error) as e:
             xg.beam_select_workspace(*bad)
