@@ -243,7 +243,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
 // from 2^-6 on).  A count of the pieces' best scores gives the bin that the n-th best of them lies in: at least n candidates lie in it or
 // below, so only pieces, in them blocks, in them tokens that do are looked at, which are few more than n as a rule.  Where they are not (fewer
 // pieces than candidates, rows that differ much), blocks, and then tokens, are counted again.  16 lanes have a row's pieces.
-constexpr int kPickThreads = 1024, kPickMostWaves = kPickThreads / 64, kPickBins = 1024, kPickListed = 1024, kPickElems = 2048, kPickHeld = 5;
+constexpr int kPickThreads = 1024, kPickMostWaves = kPickThreads / 64, kPickBins = 1024, kPickListed = 512, kPickElems = 1024, kPickHeld = 5;
 
 constexpr uint32_t kRowShift = 26, kRowBits = (1u << kRowShift) - 1;
 static_assert(kBeamsMost <= 1u << (32 - kRowShift) && ((uint64_t)kBeamVocabMost + 64 + kBeamPiece) / kBeamBlock <= kRowBits, "a row and its block fit a word");
