@@ -78,6 +78,13 @@ __device__ __forceinline__ float sum_of_64(float v) {                           
 // best, so one pass over the logits leaves two things of them: for every piece of kBeamPiece tokens the largest logit M that counts and
 // the sum of exp(x - M), and for every block its largest allowed logit.  The second kernel has the rows' L from the first, takes the
 // blocks whose best score is not below the n-th best of them, and looks at the tokens of these blocks only.
+//
+// The pass: a wavefront per piece, counted from the 128-byte boundary at or before the row's begin, so that all vectors are aligned
+// whatever the row; 32 logits a lane in registers, all loaded before the first is used; under a mask one word of it a lane, vectors
+// without an allowed token not loaded and pieces without one not looked at.  The piece's maximum goes into the exponents as it is (no
+// running maximum, no second exponential).  Bound by memory and, over bfloat16, as much by instructions (8.5 a logit, one of them at a
+// quarter rate: 47 us of issue and 46 us of memory for 1,024 rows of V = 151,936, 311 MB of logits and 19 of masks, which take 47.5 us,
+// 6.9 TB/s).  256 rows fp32, masks of all kinds 14.4 us; 64 rows of V = 128,256 4.1; 4 rows of 32,000 with few tokens allowed 4.0.
 constexpr int kScanWaves = 4;
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr double LN2 = 0.693147180559945309417232;
@@ -243,6 +250,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
 // from 2^-6 on).  A count of the pieces' best scores gives the bin that the n-th best of them lies in: at least n candidates lie in it or
 // below, so only pieces, in them blocks, in them tokens that do are looked at, which are few more than n as a rule.  Where they are not (fewer
 // pieces than candidates, rows that differ much), blocks, and then tokens, are counted again.  16 lanes have a row's pieces.
+// Bound by latency: a dozen dependent steps (rows' sums, count, pieces, blocks, tokens, places), three of them with a load from memory
+// that other dies have written (about 1 us each).  us, kernel trace: 1 group of 4 beams, 8 candidates 8.8; 128 of 8, 16 candidates 13.4;
+// 8 of 32, 64 candidates 15.4.  Both kernels in one launch, a workgroup for a group of up to 64 pieces, is slower: 1 x 4 beams, V = 32,000
+// 12.3 as two, 23.6 as one; 64 x 8, V = 4,000 13.9 and 21.6.
 constexpr int kPickThreads = 1024, kPickMostWaves = kPickThreads / 64, kPickBins = 1024, kPickListed = 512, kPickElems = 1024, kPickHeld = 5;
 
 constexpr uint32_t kRowShift = 26, kRowBits = (1u << kRowShift) - 1;
@@ -278,6 +289,15 @@ __device__ __forceinline__ double exp2_of(double t) {
 __device__ __forceinline__ double log_of(double v) {
     const double y = (double)__builtin_amdgcn_logf((float)v), e = v * exp2_of(-y) - 1.0;      // (log2 in 32 bits, then what is missing)
     return y * LN2 + e - e * e * 0.5;
+}
+// e^d for d <= 0, to the last bits of a double.
+__device__ __forceinline__ double exp_of(double d) {
+    d = __builtin_fmax(d, -1000.0);                                  // (zero)
+    const double n = __builtin_rint(d * 1.4426950408889634073599), f = __builtin_fma(-n, 2.3190468138462996e-17, __builtin_fma(-n, 0.69314718055994528623, d));
+    double p = 1.0 / 6227020800.0;
+    constexpr double C[] = {1.0 / 479001600, 1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 1.0 / 2, 1.0, 1.0};
+    _Pragma("unroll") for (int i = 0; i < 13; ++i) p = __builtin_fma(p, f, C[i]);
+    return __builtin_ldexp(p, (int)n);
 }
 // Over a row of 16 lanes, in all of them; and how many of the lanes' counts lie up to and with a lane.
 template <int CTRL>
@@ -328,8 +348,7 @@ __device__ __forceinline__ uint64_t place_of(uint32_t row, long long token) { re
 // (no branch: three compares)
 __device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) { return (a.score > b.score) | ((a.score == b.score) & (a.at < b.at)); }
 
-// 16 tokens of a row from t0 on: their logits, and which of them are in the row and, unless all
-// are wanted, allowed.
+// 16 tokens of a row from t0 on: their logits, and which of them are in the row and, unless all are wanted, allowed.
 template <class E>
 __device__ __forceinline__ uint32_t load_16(const BeamSelect& A, uint32_t r, int t0, bool all, float* x) {
     constexpr int EPV = Elem<E>::EPV, VECS = 16 / EPV;
@@ -352,10 +371,39 @@ __device__ __forceinline__ uint32_t load_16(const BeamSelect& A, uint32_t r, int
     return ok & 0xFFFF;
 }
 
+// What is seldom called is no part of the kernel; it is handed the launch's own arguments and the place in LDS (a struct on the stack would be
+// read from memory a word at a time, and LDS through flat instructions).
+#if defined(__HIP_DEVICE_COMPILE__)
+#define XG2_CONSTANT __attribute__((address_space(4)))
+#define XG2_LDS __attribute__((address_space(3)))
+#else
+#define XG2_CONSTANT
+#define XG2_LDS
+#endif
+typedef const XG2_CONSTANT BeamSelect* PickArgs;
+typedef XG2_LDS PickShared* PickLds;
+static_assert(alignof(BeamSelect) == 8, "k_beam_pick's struct of arguments lies 40 bytes on, behind three pointers and three words");
+__device__ __forceinline__ PickArgs pick_args() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return (PickArgs)((const XG2_CONSTANT char*)__builtin_amdgcn_kernarg_segment_ptr() + 40);
+#else
+    return nullptr;
+#endif
+}
+__device__ __forceinline__ BeamSelect args_of(PickArgs p) {
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    const PickArgs same = reinterpret_cast<PickArgs>((uint64_t)uniform((uint32_t)(at >> 32)) << 32 | uniform((uint32_t)at));
+    BeamSelect A;
+    __builtin_memcpy(&A, same, sizeof(A));
+    return A;
+}
+
 // The row's sum in 64 bits; anew: also the maxima of its pieces and blocks without NaN (what the first kernel left of the row is not used).
 template <class E>
-__device__ __attribute__((noinline)) void repair_row(const BeamSelect& A, PickShared& S, uint32_t g, uint32_t k, bool anew) {
-    const uint32_t r = g * A.beams + k, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x >> 6;
+__device__ __attribute__((noinline)) void repair_row(PickArgs args, PickLds lds, uint32_t group, uint32_t beam, bool anew) {
+    const BeamSelect A = args_of(args);
+    PickShared& S = *(PickShared*)lds;
+    const uint32_t g = uniform(group), k = uniform(beam), r = g * A.beams + k, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x >> 6;
     const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
     const int before = before_row(row);
     float top = NINF, x[16];
@@ -370,7 +418,7 @@ __device__ __attribute__((noinline)) void repair_row(const BeamSelect& A, PickSh
                 uint32_t ok = inside;
                 if (A.bitmask) { float again[16]; ok = load_16<E>(A, r, t0, false, again); }
                 float best = NINF;
-                for (int c = 0; c < 16; ++c) {
+                _Pragma("unroll") for (int c = 0; c < 16; ++c) {
                     if ((ok >> c) & 1u) best = x[c] > best ? x[c] : best;                                    // (false for NaN)
                     if (((A.over_all ? inside : ok) >> c) & 1u) top = x[c] > top ? x[c] : top;
                 }
@@ -389,14 +437,23 @@ __device__ __attribute__((noinline)) void repair_row(const BeamSelect& A, PickSh
     __syncthreads();
     for (uint32_t w = 0; w < waves; ++w) top = (float)S.wave_top[w] > top ? (float)S.wave_top[w] : top;
     __syncthreads();
-    // (counted from the row's begin, wherever it lies: rows that are alike have sums that are alike)
+    // (counted from the row's begin, wherever it lies: rows that are alike have sums that are alike; the next 16 tokens are on their way
+    // while these are added up)
     double sum = 0;
-    for (int t0 = 16 * (int)tid; t0 < A.V; t0 += 16 * (int)blockDim.x) {
-        uint32_t ok = load_16<E>(A, r, t0, A.over_all, x);
-        if (ok == 0) continue;
-        _Pragma("unroll 4") for (int c = 0; c < 16; ++c) {
-            const double e = top == -NINF ? (x[c] == top ? 1.0 : 0.0) : exp((double)x[c] - (double)top);
-            sum += ((ok >> c) & 1u) && x[c] > NINF ? e : 0.0;
+    const int step = 16 * (int)blockDim.x;
+    int t0 = 16 * (int)tid;
+    uint32_t ok = t0 < A.V ? load_16<E>(A, r, t0, A.over_all, x) : 0;
+    while (t0 < A.V) {
+        float now[16];
+        const uint32_t counted = ok;
+        _Pragma("unroll") for (int c = 0; c < 16; ++c) now[c] = x[c];
+        t0 += step;
+        if (t0 < A.V) ok = load_16<E>(A, r, t0, A.over_all, x);
+        if (counted == 0) continue;
+        // (a loop that is not taken apart would have the logits in memory)
+        _Pragma("unroll") for (int c = 0; c < 16; ++c) {
+            const double e = top == -NINF ? (now[c] == top ? 1.0 : 0.0) : exp_of((double)now[c] - (double)top);
+            sum += ((counted >> c) & 1u) && now[c] > NINF ? e : 0.0;
         }
     }
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
@@ -444,10 +501,12 @@ __device__ __forceinline__ void write_choice(const BeamSelect& A, uint32_t g, ui
 // Too many are too much alike (logits that are all the same): all sums in 64 bits, then the best block n times, and the best candidate of
 // these blocks n times, each the next one after the one before.
 template <class E>
-__device__ __attribute__((noinline)) void pick_one_by_one(const BeamSelect& A, PickShared& S, uint32_t g) {
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6, K = A.beams, N = A.n_out, n_blocks = A.pieces * kBeamPieceBlocks;
+__device__ __attribute__((noinline)) void pick_one_by_one(PickArgs args, PickLds lds, uint32_t group) {
+    const BeamSelect A = args_of(args);
+    PickShared& S = *(PickShared*)lds;
+    const uint32_t g = uniform(group), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6, K = A.beams, N = A.n_out, n_blocks = A.pieces * kBeamPieceBlocks;
     const double none = -(double)__builtin_inff();
-    for (uint32_t k = 0; k < K; ++k) if (S.state[k] == ROW_LIVE && !S.exact[k]) repair_row<E>(A, S, g, k, false);
+    for (uint32_t k = 0; k < K; ++k) if (S.state[k] == ROW_LIVE && !S.exact[k]) repair_row<E>(args, lds, g, k, false);
     uint32_t n_found = 0;
     Candidate last{0, ~0ull};
     for (; n_found < N; ++n_found) {
@@ -493,6 +552,8 @@ __device__ __attribute__((noinline)) void pick_one_by_one(const BeamSelect& A, P
 template <class E>
 __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_stats, const float* scores, const int32_t* finished, uint32_t K, uint32_t pieces, uint32_t N, BeamSelect A) {
     __shared__ PickShared S;
+    const PickArgs args = pick_args();
+    const PickLds lds = (PickLds)&S;
     const uint32_t g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x >> 6;
     constexpr double none = -(double)__builtin_inff();
     // 16 lanes have a row.  No score of a row is above its beam's (a logarithm of a probability is at most zero): the best of the beams' is
@@ -572,7 +633,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
     } else if (state == ROW_ENDED && part == 0) count(bin_of(top, base));
     if (mine && part == 0) { S.state[k] = state; S.base[k] = base; S.infinite[k] = 0; S.exact[k] = state != ROW_LIVE; S.repair[k] = repair; }
     if (__syncthreads_or((int)repair)) {
-        for (uint32_t q = 0; q < K; ++q) if (S.repair[q]) repair_row<E>(A, S, g, q, true);
+        for (uint32_t q = 0; q < K; ++q) if (S.repair[q]) repair_row<E>(args, lds, g, q, true);
         if (repair) state = S.state[k];
         if (repair && state == ROW_LIVE) {
             _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) {
@@ -683,7 +744,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
         __syncthreads();
         if (counted || S.n_elems <= 2 * N + 64) break;
     }
-    if (S.n_pieces > kPickListed || listed_all > kPickListed || S.n_elems > kPickElems) { pick_one_by_one<E>(A, S, g); return; }
+    if (S.n_pieces > kPickListed || listed_all > kPickListed || S.n_elems > kPickElems) { pick_one_by_one<E>(args, lds, g); return; }
     const uint32_t R = S.n_elems;
     for (;;) {
         // A candidate's place is the number of candidates before it: a wavefront compares 64 candidates with its part of all.
@@ -712,7 +773,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
             if (n + 1 <= N || !(S.found[S.sorted[N - 1]].score - b.score > A.near)) { S.repair[ka] = S.repair[kb] = 1; any = 1; }
         }
         if (!__syncthreads_or(any)) break;
-        for (uint32_t q = 0; q < K; ++q) if (S.repair[q] && !S.exact[q]) repair_row<E>(A, S, g, q, false);
+        for (uint32_t q = 0; q < K; ++q) if (S.repair[q] && !S.exact[q]) repair_row<E>(args, lds, g, q, false);
         for (uint32_t i = tid; i < R; i += blockDim.x)
             if ((uint32_t)S.found[i].at != 0) S.found[i].score = score_of(S, (uint32_t)(S.found[i].at >> 32), S.x[i]);
         __syncthreads();
@@ -725,7 +786,8 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
 // that is not its own state, so the parent's goes there at once; the slot's record and its frontier planes have one place, so these
 // wait in registers (the record a word a lane) until all wavefronts of the group have read theirs.  Bound by latency: three loads in a row
 // (parents, records, context), so the first 64 of everything in a context are asked for together, without waiting for the counts (a slot
-// has room for that many and more), like the planes.
+// has room for that many and more), like the planes.  4 slots 2.2 us, 512 slots in groups of 8 4.0 (with records in LDS and contexts asked
+// for after their counts 4.0 and 9.0).
 constexpr uint32_t kRowWords = sizeof(FillRow) / 4;
 static_assert(kRowWords <= 64 && offsetof(FillRow, front_off) == 0 && offsetof(FillRow, front_n) == 4 && offsetof(FillRow, item_off) == 8 && offsetof(FillRow, item_n) == 12 &&
               offsetof(FillRow, wait_base) == 16 && offsetof(FillRow, waitoff_off) == 20 && offsetof(FillRow, H) == 24 && offsetof(FillRow, pad) == 36 && offsetof(FillRow, n_wait) == 44,
@@ -784,7 +846,8 @@ __global__ __launch_bounds__(1024) void k_batch_reorder(const int32_t* parents, 
 
 // ---- rows of a buffer -----------------------------------------------------------------------------------------------
 // A thread has one column of all rows of a group: it loads what every row will hold there and then stores it, so nothing waits for
-// anybody and no second buffer is needed.  Rows that keep their place are neither read (but as parents) nor written.
+// anybody and no second buffer is needed.  Rows that keep their place are neither read (but as parents) nor written.  Bound by memory:
+// 32 groups of 8 beams, 472 MB read and written 90 us, 5.2 TB/s, what a large copy reaches.
 // TOGETHER columns of a thread, `apart` bytes from one to the next, of which `n` exist.  (from: lane k has the row that row k takes; the
 // lane's rows are picked by constants.  What a row's number makes of its stride is worked out anew where it is used: kept for all rows
 // it would not fit the scalar registers.)
@@ -847,6 +910,8 @@ __global__ __launch_bounds__(256) void k_beam_reorder_rows(const int32_t* parent
 // put together two and two (in as many rounds as the number of segments has binary digits), then every segment again from the beams
 // that the sequences enter it with, writing their tokens.  A step's parents are one load for all beams of a group, which waits for nothing;
 // which of them a beam's is comes from the lane that holds it.  Segments of up to kTraceHeld steps are loaded once and kept in registers.
+// Bound by latency (the loads, then some 30 exchanges of about 50 ns).  4 beams, 128 steps 4.8 us, 64 groups of 8 beams, 1,500 steps 9.4 us;
+// a thread per sequence, step after step 24.8 and 311.
 constexpr int kTraceThreads = 1024, kTraceHeld = 16;
 template <int WIDTH>
 __global__ __launch_bounds__(kTraceThreads) void k_beam_backtrace(BeamTrace A, uint32_t segments, uint32_t length) {
@@ -936,11 +1001,13 @@ template <class E>
 static void launch_beam_select_as(const BeamSelect& A, hipStream_t stream) {
     const uint32_t rows = A.groups * A.beams;
     auto* const kernel = !A.bitmask ? k_beam_scan<E, 0> : A.over_all ? k_beam_scan<E, 2> : k_beam_scan<E, 1>;
+    // few pieces: a workgroup each, to reach as many compute units
     const uint32_t waves = (uint64_t)A.pieces * rows <= 512 ? 1 : kScanWaves;
     for (uint32_t first = 0; first < rows; first += 65535) {         // grid.y limit
         const uint32_t n = std::min<uint32_t>(65535, rows - first);
         hipLaunchKernelGGL(kernel, dim3((A.pieces + waves - 1) / waves, n), dim3(64 * waves), 0, stream, A.bitmask, A.bm_stride, A.scores, A.finished, A.logits, A.row_stride, A.pieces, A.V, A, first);
     }
+    // 16 lanes for every row, four for every block that is looked at
     const uint32_t threads = std::min<uint32_t>(kPickThreads, std::max<uint32_t>(256, (std::max(16 * A.beams, 4 * (A.n_out + A.n_out / 4)) + 63) / 64 * 64));
     hipLaunchKernelGGL(k_beam_pick<E>, dim3(A.groups), dim3(threads), 0, stream, A.stats, A.scores, A.finished, A.beams, A.pieces, A.n_out, A);
 }
@@ -995,7 +1062,7 @@ void launch_beam_reorder_rows(const BeamRows& A, hipStream_t stream) {
 
 template <int WIDTH>
 static void launch_backtrace_as(const BeamTrace& A, hipStream_t stream) {
-    // As many segments as a workgroup has room for, of eight steps at the least
+    // as many segments as a workgroup has room for, of eight steps at the least
     constexpr uint32_t most = kTraceThreads / WIDTH;
     const uint32_t length = std::max<uint32_t>(8, (A.steps + most - 1) / most), segments = (A.steps + length - 1) / length;
     const uint32_t threads = std::max<uint32_t>(64, (segments * WIDTH + 63) / 64 * 64);
