@@ -264,6 +264,7 @@ enum RowState : uint32_t { ROW_NONE, ROW_LIVE, ROW_ENDED };
 struct alignas(16) Candidate { double score; uint64_t at; };
 struct PickShared {
     double base[kBeamsMost];                   // score of a token of the row: base + its logit (infinite: base, where the logit is +inf)
+    float largest[kBeamsMost];                 // of the row's logits that count, from the first kernel
     uint32_t state[kBeamsMost];
     uint32_t infinite[kBeamsMost], exact[kBeamsMost], repair[kBeamsMost];
     double wave_top[kPickMostWaves];
@@ -348,28 +349,33 @@ __device__ __forceinline__ uint64_t place_of(uint32_t row, long long token) { re
 // (no branch: three compares)
 __device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) { return (a.score > b.score) | ((a.score == b.score) & (a.at < b.at)); }
 
-// 16 tokens of a row from t0 on: their logits, and which of them are in the row and, unless all are wanted, allowed.
+// 16 tokens of a row from t0 on: asked for, and taken when they are there: their logits, and which of them are in the row and, unless all
+// are wanted, allowed.
 template <class E>
-__device__ __forceinline__ uint32_t load_16(const BeamSelect& A, uint32_t r, int t0, bool all, float* x) {
-    constexpr int EPV = Elem<E>::EPV, VECS = 16 / EPV;
-    const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
-    const bool inner = t0 >= 0 && t0 + 16 <= A.V;
+struct Sixteen {
+    static constexpr int EPV = Elem<E>::EPV, VECS = 16 / EPV;
     Vec4 raw[VECS];
-    uint32_t ok = 0xFFFF;
-    if (A.bitmask && !all) {
-        const Global<const uint32_t> bm = (Global<const uint32_t>)(A.bitmask + (long long)r * A.bm_stride);
-        const int at = t0 >> 5, last = (A.V - 1) >> 5;               // (an arithmetic shift: rounds down)
-        ok = (uint32_t)(((uint64_t)bm[min(max(at + 1, 0), last)] << 32 | bm[min(max(at, 0), last)]) >> (t0 & 31));
+    uint32_t word, next;
+    __device__ __forceinline__ void ask(const BeamSelect& A, uint32_t r, int t0, bool all) {
+        const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
+        word = next = ~0u;
+        if (A.bitmask && !all) {
+            const Global<const uint32_t> bm = (Global<const uint32_t>)(A.bitmask + (long long)r * A.bm_stride);
+            const int at = t0 >> 5, last = (A.V - 1) >> 5;           // (an arithmetic shift: rounds down)
+            word = bm[min(max(at, 0), last)];
+            next = bm[min(max(at + 1, 0), last)];
+        }
+        if (t0 >= 0 && t0 + 16 <= A.V) { _Pragma("unroll") for (int v = 0; v < VECS; ++v) raw[v] = ((Global<const Wide4>)(row + t0))[v]; }
+        else { _Pragma("unroll") for (int v = 0; v < VECS; ++v) raw[v] = Elem<E>::gather(row, t0 + v * EPV, A.V); }
     }
-    if (inner) { _Pragma("unroll") for (int v = 0; v < VECS; ++v) raw[v] = ((Global<const Wide4>)(row + t0))[v]; }
-    else {
-        _Pragma("unroll") for (int v = 0; v < VECS; ++v) raw[v] = Elem<E>::gather(row, t0 + v * EPV, A.V);
+    __device__ __forceinline__ uint32_t take(int V, int t0, float* x) const {
+        uint32_t ok = (uint32_t)(((uint64_t)next << 32 | word) >> (t0 & 31)) & 0xFFFF;
         if (t0 < 0) ok &= 0xFFFFu << min(-t0, 16);
-        if (t0 + 16 > A.V) ok &= t0 < A.V ? 0xFFFFu >> (t0 + 16 - A.V) : 0u;
+        if (t0 + 16 > V) ok &= t0 < V ? 0xFFFFu >> (t0 + 16 - V) : 0u;
+        _Pragma("unroll") for (int v = 0; v < VECS; ++v) Elem<E>::unpack(raw[v], x + v * EPV);
+        return ok;
     }
-    _Pragma("unroll") for (int v = 0; v < VECS; ++v) Elem<E>::unpack(raw[v], x + v * EPV);
-    return ok & 0xFFFF;
-}
+};
 
 // What is seldom called is no part of the kernel; it is handed the launch's own arguments and the place in LDS (a struct on the stack would be
 // read from memory a word at a time, and LDS through flat instructions).
@@ -407,6 +413,7 @@ __device__ __attribute__((noinline)) void repair_row(PickArgs args, PickLds lds,
     const E* const row = static_cast<const E*>(A.logits) + (long long)r * A.row_stride;
     const int before = before_row(row);
     float top = NINF, x[16];
+    const float score = ((Global<const float>)A.scores)[r];
     __syncthreads();                                                 // (S.wave_top has been read by all)
     if (anew) {
         // four lanes have a block, a wavefront in two turns a piece
@@ -414,9 +421,11 @@ __device__ __attribute__((noinline)) void repair_row(PickArgs args, PickLds lds,
             float piece_best = NINF;
             for (uint32_t b = lane >> 2; b < kBeamPieceBlocks; b += 16) {
                 const int t0 = (int)p * kBeamPiece + (int)b * kBeamBlock + 16 * (int)(lane & 3) - before;
-                const uint32_t inside = load_16<E>(A, r, t0, true, x);
-                uint32_t ok = inside;
-                if (A.bitmask) { float again[16]; ok = load_16<E>(A, r, t0, false, again); }
+                Sixteen<E> T;
+                T.ask(A, r, t0, false);
+                const uint32_t ok = T.take(A.V, t0, x);
+                T.word = T.next = ~0u;
+                const uint32_t inside = T.take(A.V, t0, x);
                 float best = NINF;
                 _Pragma("unroll") for (int c = 0; c < 16; ++c) {
                     if ((ok >> c) & 1u) best = x[c] > best ? x[c] : best;                                    // (false for NaN)
@@ -429,31 +438,29 @@ __device__ __attribute__((noinline)) void repair_row(PickArgs args, PickLds lds,
             for (int d = 4; d < 64; d *= 2) { const float o = __shfl_xor(piece_best, d); piece_best = o > piece_best ? o : piece_best; }
             if (lane == 0) ((Global<float>)(A.stats + ((size_t)r * A.pieces + p)))[2] = piece_best;
         }
-    } else {
-        for (uint32_t p = tid; p < A.pieces; p += blockDim.x) { const float o = ((Global<const float>)(A.stats + ((size_t)r * A.pieces + p)))[0]; top = o > top ? o : top; }
-    }
-    for (int d = 1; d < 64; d *= 2) { const float o = __shfl_xor(top, d); top = o > top ? o : top; }
-    if (lane == 0) S.wave_top[wave] = top;
-    __syncthreads();
-    for (uint32_t w = 0; w < waves; ++w) top = (float)S.wave_top[w] > top ? (float)S.wave_top[w] : top;
-    __syncthreads();
-    // (counted from the row's begin, wherever it lies: rows that are alike have sums that are alike; the next 16 tokens are on their way
-    // while these are added up)
+        for (int d = 1; d < 64; d *= 2) { const float o = __shfl_xor(top, d); top = o > top ? o : top; }
+        if (lane == 0) S.wave_top[wave] = top;
+        __syncthreads();
+        for (uint32_t w = 0; w < waves; ++w) top = (float)S.wave_top[w] > top ? (float)S.wave_top[w] : top;
+        __syncthreads();
+    } else top = S.largest[k];
+    // (counted from the row's begin, wherever it lies: rows that are alike have sums that are alike; the tokens of the next turn are on
+    // their way)
     double sum = 0;
     const int step = 16 * (int)blockDim.x;
+    Sixteen<E> one, two;
     int t0 = 16 * (int)tid;
-    uint32_t ok = t0 < A.V ? load_16<E>(A, r, t0, A.over_all, x) : 0;
-    while (t0 < A.V) {
-        float now[16];
-        const uint32_t counted = ok;
-        _Pragma("unroll") for (int c = 0; c < 16; ++c) now[c] = x[c];
-        t0 += step;
-        if (t0 < A.V) ok = load_16<E>(A, r, t0, A.over_all, x);
+    if (t0 < A.V) one.ask(A, r, t0, A.over_all);
+    if (t0 + step < A.V) two.ask(A, r, t0 + step, A.over_all);
+    for (; t0 < A.V; t0 += step) {
+        const uint32_t counted = one.take(A.V, t0, x);
+        one = two;
+        if (t0 + 2 * step < A.V) two.ask(A, r, t0 + 2 * step, A.over_all);
         if (counted == 0) continue;
         // (a loop that is not taken apart would have the logits in memory)
         _Pragma("unroll") for (int c = 0; c < 16; ++c) {
-            const double e = top == -NINF ? (now[c] == top ? 1.0 : 0.0) : exp_of((double)now[c] - (double)top);
-            sum += ((counted >> c) & 1u) && now[c] > NINF ? e : 0.0;
+            const double e = top == -NINF ? (x[c] == top ? 1.0 : 0.0) : exp_of((double)x[c] - (double)top);
+            sum += ((counted >> c) & 1u) && x[c] > NINF ? e : 0.0;
         }
     }
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
@@ -466,7 +473,7 @@ __device__ __attribute__((noinline)) void repair_row(PickArgs args, PickLds lds,
         if (top == NINF) S.state[k] = ROW_NONE;
         else {
             S.infinite[k] = top == -NINF;
-            S.base[k] = (double)A.scores[r] - (log(all) + (top == -NINF ? 0.0 : (double)top));
+            S.base[k] = (double)score - (log(all) + (top == -NINF ? 0.0 : (double)top));
         }
     }
     __threadfence_block();
@@ -588,8 +595,9 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
         return m > NINF && v > none ? bin_of(top, v) : (uint32_t)kPickBins;
     };
     auto count = [&](uint32_t b) { if (b < kPickBins) atomicAdd(&S.bins[bin_at(b)], 1u); };
+    float largest = NINF;
     if (state == ROW_LIVE) {
-        float m = NINF;
+        float& m = largest;
         bool odd = false;
         auto look = [&](const Vec4& v) {
             const float x = __uint_as_float(v[0]), y = __uint_as_float(v[1]);
@@ -631,7 +639,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
             }
         }
     } else if (state == ROW_ENDED && part == 0) count(bin_of(top, base));
-    if (mine && part == 0) { S.state[k] = state; S.base[k] = base; S.infinite[k] = 0; S.exact[k] = state != ROW_LIVE; S.repair[k] = repair; }
+    if (mine && part == 0) { S.state[k] = state; S.base[k] = base; S.infinite[k] = 0; S.exact[k] = state != ROW_LIVE; S.repair[k] = repair; S.largest[k] = largest; }
     if (__syncthreads_or((int)repair)) {
         for (uint32_t q = 0; q < K; ++q) if (S.repair[q]) repair_row<E>(args, lds, g, q, true);
         if (repair) state = S.state[k];
@@ -714,7 +722,9 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
             const uint32_t block = S.blocks[i], row_k = block >> kRowShift, row_r = g * K + row_k;
             const int t0 = (int)((block & kRowBits) * kBeamBlock + 16 * (tid & 3)) - before_row(static_cast<const E*>(A.logits) + (long long)row_r * A.row_stride);
             float x[16];
-            const uint32_t ok = load_16<E>(A, row_r, t0, false, x);
+            Sixteen<E> T;
+            T.ask(A, row_r, t0, false);
+            const uint32_t ok = T.take(A.V, t0, x);
             // a bound in 32 bits first
             const double least = reach - S.base[row_k];
             const float bound = (float)least - (__builtin_fabsf((float)least) * 1e-6f + 1e-3f);
