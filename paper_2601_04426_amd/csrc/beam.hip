@@ -137,7 +137,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
     // (the first 14 words of arguments are in registers when the kernel starts, a struct's are loaded)
     constexpr int EPV = Elem<E>::EPV, STEPS = kBeamPiece / 64 / EPV, VPW = 32 / EPV, LANES = kBeamBlock / EPV;   // vectors of a mask word, lanes of a block
     constexpr uint32_t ALL = (1u << EPV) - 1;
-    const uint32_t r = first_row + blockIdx.y, lane = threadIdx.x & 63, piece = blockIdx.x * (blockDim.x >> 6) + uniform(threadIdx.x >> 6);
+    const uint32_t r = first_row + blockIdx.y, lane = threadIdx.x & 63, piece = blockIdx.x * kScanWaves + uniform(threadIdx.x >> 6);
     if (piece >= pieces) return;
     const E* const row = static_cast<const E*>(logits) + (long long)r * row_stride;
     const int e0 = (int)piece * kBeamPiece - before_row(row);             
@@ -1011,11 +1011,9 @@ template <class E>
 static void launch_beam_select_as(const BeamSelect& A, hipStream_t stream) {
     const uint32_t rows = A.groups * A.beams;
     auto* const kernel = !A.bitmask ? k_beam_scan<E, 0> : A.over_all ? k_beam_scan<E, 2> : k_beam_scan<E, 1>;
-    // few pieces: a workgroup each, to reach as many compute units
-    const uint32_t waves = (uint64_t)A.pieces * rows <= 512 ? 1 : kScanWaves;
     for (uint32_t first = 0; first < rows; first += 65535) {         // grid.y limit
         const uint32_t n = std::min<uint32_t>(65535, rows - first);
-        hipLaunchKernelGGL(kernel, dim3((A.pieces + waves - 1) / waves, n), dim3(64 * waves), 0, stream, A.bitmask, A.bm_stride, A.scores, A.finished, A.logits, A.row_stride, A.pieces, A.V, A, first);
+        hipLaunchKernelGGL(kernel, dim3((A.pieces + kScanWaves - 1) / kScanWaves, n), dim3(64 * kScanWaves), 0, stream, A.bitmask, A.bm_stride, A.scores, A.finished, A.logits, A.row_stride, A.pieces, A.V, A, first);
     }
     // 16 lanes for every row, four for every block that is looked at
     const uint32_t threads = std::min<uint32_t>(kPickThreads, std::max<uint32_t>(256, (std::max(16 * A.beams, 4 * (A.n_out + A.n_out / 4)) + 63) / 64 * 64));
