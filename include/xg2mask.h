@@ -350,7 +350,8 @@ int32_t xg2_batch_reorder(xg2_batch*, int32_t beams, const int32_t* parents_dev,
  * layers and pieces = heads, [layers, rows, positions, heads, width] outer = layers, pieces = 1 and position_bytes of all heads.
  * begin_dev, end_dev (device, G int32 each, may be NULL: 0 and positions): only positions begin[g] <= t < end[g] of group g's
  * rows are touched (its beams have the prompt in common); values outside 0 .. positions count as these.  Pieces must not
- * overlap, and there are at most 2^23 of them in a row.  parents_dev: device, G * K int32, each in its row's group; rows with -1, or any row outside the group, stay.    */
+ * overlap, and there are at most 2^23 of them in a row.  parents_dev: device, G * K int32, each in its row's group; rows with
+ * -1, or with any row outside the group, stay.                                                                             */
 int32_t xg2_beam_reorder_rows(void* data_dev, int32_t groups, int32_t beams, const int32_t* parents_dev, int64_t row_stride,
                               int32_t outer, int64_t outer_stride, int32_t pieces, int64_t piece_stride, int32_t positions,
                               int64_t position_bytes, const int32_t* begin_dev, const int32_t* end_dev, void* hip_stream);
@@ -358,7 +359,8 @@ int32_t xg2_beam_reorder_rows(void* data_dev, int32_t groups, int32_t beams, con
 /* The sequences of all beams after `steps` steps: tokens_dev and parents_dev hold what the steps chose, step t at t * step_stride
  * (G * K int32 each).  Row r of out_tokens_dev (out_stride int32 from one to the next) receives steps tokens: that of row r at the
  * last step, of its parent at the step before, and so on.  Where the way leaves the group (a parent of -1, or any outside) the
- * steps before are -1.  out_lengths_dev (may be NULL): per row, steps up to and with the last token that is not negative.    */
+ * steps before are -1.  out_lengths_dev (may be NULL): per row, steps up to and with the last token that is not negative.
+ * No output may overlap an input.                                                                                          */
 int32_t xg2_beam_backtrace(const int32_t* tokens_dev, const int32_t* parents_dev, int32_t steps, int64_t step_stride, int32_t groups,
                            int32_t beams, int32_t* out_tokens_dev, int64_t out_stride, int32_t* out_lengths_dev, void* hip_stream);
 

@@ -35,11 +35,6 @@ __device__ __forceinline__ float moved(float own, float v) { return __int_as_flo
 // from memory, to make signalling NaN quiet ones; where one of these is met the sum of exponentials is NaN, which is looked for.)
 __device__ __forceinline__ float larger(float a, float b) { float d; asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b)); return d; }
 __device__ __forceinline__ float larger(float a, float b, float c) { float d; asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c)); return d; }
-#if defined(__HIP_DEVICE_COMPILE__)
-#define READABLE(v) asm volatile("s_nop 1" : "+v"(v))                // what inline assembly wrote, before another lane reads it
-#else
-#define READABLE(v) (void)0
-#endif
 // Four values at a time, stage by stage, so that none is read across lanes within two instructions of being written (which the device does
 // not wait for, and of which the compiler knows nothing here).
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -251,9 +246,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
 // below, so only pieces, in them blocks, in them tokens that do are looked at, which are few more than n as a rule.  Where they are not (fewer
 // pieces than candidates, rows that differ much), blocks, and then tokens, are counted again.  16 lanes have a row's pieces.
 // Bound by latency: a dozen dependent steps (rows' sums, count, pieces, blocks, tokens, places), three of them with a load from memory
-// that other dies have written (about 1 us each).  us, kernel trace: 1 group of 4 beams, 8 candidates 8.8; 128 of 8, 16 candidates 13.4;
-// 8 of 32, 64 candidates 15.4.  Both kernels in one launch, a workgroup for a group of up to 64 pieces, is slower: 1 x 4 beams, V = 32,000
-// 12.3 as two, 23.6 as one; 64 x 8, V = 4,000 13.9 and 21.6.
+// that other dies have written (about 1 us each).  us, kernel trace: 1 group of 4 beams, V = 32,000, 8 candidates 6.9; 16 of 4, V = 128,256,
+// 4 candidates 8.6; 128 of 8, V = 151,936, 16 candidates 9.5; 8 of 32, V = 151,936, 64 candidates 11.8.  Both kernels in one launch, a workgroup
+// for a group of up to 64 pieces, was slower when it was tried: 1 x 4 beams, V = 32,000 12.3 as two, 23.6 as one; 64 x 8, V = 4,000 13.9 and 21.6.
 constexpr int kPickThreads = 1024, kPickMostWaves = kPickThreads / 64, kPickBins = 1024, kPickListed = 512, kPickElems = 1024, kPickHeld = 5;
 
 constexpr uint32_t kRowShift = 26, kRowBits = (1u << kRowShift) - 1;
