@@ -558,8 +558,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
     const PickLds lds = (PickLds)&S;
     const uint32_t g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x >> 6;
     constexpr double none = -(double)__builtin_inff();
-    // 16 lanes have a row.  No score of a row is above its beam's (a logarithm of a probability is at most zero): the best of the beams' is
-    // what distances are taken from, and is known before the sums are.
+    // 16 lanes have a row.
     const uint32_t k = tid >> 4, part = tid & 15, r = g * K + k;
     const Global<const Vec4> stats = (Global<const Vec4>)(all_stats + (size_t)r * pieces);
     const bool mine = k < K;
@@ -574,22 +573,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
     for (uint32_t i = tid; i < kPickBins; i += blockDim.x) S.bins[i] = 0;
     if (tid == 0) S.n_pieces = S.n_blocks = S.n_elems = 0;
     uint32_t state = !(s > NINF && s < -NINF) ? ROW_NONE : ended != 0 ? ROW_ENDED : ROW_LIVE, repair = 0;
-    {
-        float m = state == ROW_NONE ? NINF : s;
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32));
-        if (lane == 0) S.wave_top[wave] = m;
-    }
-    __syncthreads();
-    double top = none, base = s;
-    for (uint32_t w = 0; w < waves; ++w) top = S.wave_top[w] > top ? S.wave_top[w] : top;
-    // how many pieces (and ended beams) have their best score in each bin
-    uint32_t bin[kPickHeld];
-    auto bin_if = [&](uint32_t row, float m) {
-        const double v = score_of(S, row, m);
-        return m > NINF && v > none ? bin_of(top, v) : (uint32_t)kPickBins;
-    };
-    auto count = [&](uint32_t b) { if (b < kPickBins) atomicAdd(&S.bins[bin_at(b)], 1u); };
+    double base = s;
     float largest = NINF;
     if (state == ROW_LIVE) {
         float& m = largest;
@@ -624,29 +608,53 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
         if (!repair) {
             if (m == NINF) state = ROW_NONE;
             else base -= log_of(sum) + mc * LN2;
-            _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) {
-                bin[i] = best[i] > NINF ? bin_of(top, base + best[i]) : (uint32_t)kPickBins;
-                count(bin[i]);
-            }
-            for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) {
-                const float o = ((Global<const float>)(stats + p))[2];
-                if (o > NINF) count(bin_of(top, base + o));
-            }
         }
-    } else if (state == ROW_ENDED && part == 0) count(bin_of(top, base));
+    }
     if (mine && part == 0) { S.state[k] = state; S.base[k] = base; S.infinite[k] = 0; S.exact[k] = state != ROW_LIVE; S.repair[k] = repair; S.largest[k] = largest; }
+    // Distances are taken from the best candidate: the best beam's score would do while few candidates lie as far from it as the n-th, but
+    // where a row's logits are nearly the same all tokens are as far from it.
+    bool infinite = false;
+    auto own_score = [&](float m) { return infinite ? (m == -NINF ? base : none) : base + (double)m; };
+    auto find_top = [&] {
+        double t = state == ROW_ENDED ? base : none;
+        if (state == ROW_LIVE) {
+            float m = NINF;
+            _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) m = best[i] > m ? best[i] : m;
+            for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) { const float o = ((Global<const float>)(stats + p))[2]; m = o > m ? o : m; }
+            m = largest_of_16(m);
+            if (m > NINF) t = own_score(m);
+        }
+        double o = __shfl_xor(t, 16);
+        t = o > t ? o : t;
+        o = __shfl_xor(t, 32);
+        t = o > t ? o : t;
+        if (lane == 0) S.wave_top[wave] = t;
+    };
+    find_top();
     if (__syncthreads_or((int)repair)) {
         for (uint32_t q = 0; q < K; ++q) if (S.repair[q]) repair_row<E>(args, lds, g, q, true);
-        if (repair) state = S.state[k];
-        if (repair && state == ROW_LIVE) {
-            _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) {
-                bin[i] = part + i * 16 < pieces ? bin_if(k, ((Global<const float>)(stats + part + i * 16))[2]) : (uint32_t)kPickBins;
-                count(bin[i]);
-            }
-            for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) count(bin_if(k, ((Global<const float>)(stats + p))[2]));
+        if (repair) {
+            state = S.state[k]; base = S.base[k]; infinite = S.infinite[k] != 0;
+            _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) best[i] = part + i * 16 < pieces ? ((Global<const float>)(stats + part + i * 16))[2] : NINF;
         }
+        find_top();
         __syncthreads();
     }
+    double top = none;
+    for (uint32_t w = 0; w < waves; ++w) top = S.wave_top[w] > top ? S.wave_top[w] : top;
+    // how many pieces (and ended beams) have their best score in each bin
+    uint32_t bin[kPickHeld];
+    auto bin_if = [&](uint32_t row, float m) {
+        const double v = score_of(S, row, m);
+        return m > NINF && v > none ? bin_of(top, v) : (uint32_t)kPickBins;
+    };
+    auto count = [&](uint32_t b) { if (b < kPickBins) atomicAdd(&S.bins[bin_at(b)], 1u); };
+    if (state == ROW_LIVE) {
+        auto own_bin = [&](float m) { return m > NINF && own_score(m) > none ? bin_of(top, own_score(m)) : (uint32_t)kPickBins; };
+        _Pragma("unroll") for (int i = 0; i < kPickHeld; ++i) { bin[i] = own_bin(best[i]); count(bin[i]); }
+        for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) count(own_bin(((Global<const float>)(stats + p))[2]));
+    } else if (state == ROW_ENDED && part == 0) count(bin_of(top, base));
+    __syncthreads();
     // The bin of the n-th best of what was counted (every wavefront for itself), one more: what lies within A.near of it; if fewer were counted, the last.
     auto bin_of_nth = [&] {
         uint32_t n[16], sum = 0;
