@@ -286,14 +286,29 @@ __device__ __forceinline__ double log_of(double v) {
     const double y = (double)__builtin_amdgcn_logf((float)v), e = v * exp2_of(-y) - 1.0;      // (log2 in 32 bits, then what is missing)
     return y * LN2 + e - e * e * 0.5;
 }
-// e^d for d <= 0, to the last bits of a double.
-__device__ __forceinline__ double exp_of(double d) {
-    d = __builtin_fmax(d, -1000.0);                                  // (zero)
-    const double n = __builtin_rint(d * 1.4426950408889634073599), f = __builtin_fma(-n, 2.3190468138462996e-17, __builtin_fma(-n, 0.69314718055994528623, d));
-    double p = 1.0 / 6227020800.0;
-    constexpr double C[] = {1.0 / 479001600, 1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 1.0 / 2, 1.0, 1.0};
-    _Pragma("unroll") for (int i = 0; i < 13; ++i) p = __builtin_fma(p, f, C[i]);
-    return __builtin_ldexp(p, (int)n);
+// a * b + c for a constant c that stays in its registers (the compiler's own choice adds to c in place, and copies it for every use).
+__device__ __forceinline__ double fma_const(double a, double b, double c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    double d;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+#else
+    return a * b + c;
+#endif
+}
+// The sum of e^d over four d <= 0, each to the last bits of a double: side by side, since a step waits for the one before it and a
+// workgroup has a wavefront or two on a unit.
+__device__ __forceinline__ double sum_of_exps(const double (&x)[4]) {
+    double n[4], f[4], p[4];
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) f[i] = __builtin_fmax(x[i], -1000.0);                 // (zero)
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) n[i] = __builtin_rint(f[i] * 1.4426950408889634073599);
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) f[i] = __builtin_fma(-n[i], 0.69314718055994528623, f[i]);
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) f[i] = __builtin_fma(-n[i], 2.3190468138462996e-17, f[i]);
+    constexpr double C[] = {1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 1.0 / 2, 1.0, 1.0};
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) p[i] = 1.0 / 479001600;                               // (|f| <= 0.35: the next term is 2^-52)
+    _Pragma("unroll") for (int t = 0; t < 12; ++t) _Pragma("unroll") for (int i = 0; i < 4; ++i) p[i] = fma_const(p[i], f[i], C[t]);
+    _Pragma("unroll") for (int i = 0; i < 4; ++i) p[i] = __builtin_ldexp(p[i], (int)n[i]);
+    return (p[0] + p[1]) + (p[2] + p[3]);
 }
 // Over a row of 16 lanes, in all of them; and how many of the lanes' counts lie up to and with a lane.
 template <int CTRL>
@@ -441,6 +456,8 @@ __device__ __attribute__((noinline)) void repair_row(PickArgs args, PickLds lds,
     } else top = S.largest[k];
     // (counted from the row's begin, wherever it lies: rows that are alike have sums that are alike; the tokens of the next turn are on
     // their way)
+    const bool infinite = top == -NINF;                              // (the tokens that have it count one, the others nothing)
+    const double from = infinite ? 0.0 : (double)top;
     double sum = 0;
     const int step = 16 * (int)blockDim.x;
     Sixteen<E> one, two;
@@ -452,10 +469,16 @@ __device__ __attribute__((noinline)) void repair_row(PickArgs args, PickLds lds,
         one = two;
         if (t0 + 2 * step < A.V) two.ask(A, r, t0 + 2 * step, A.over_all);
         if (counted == 0) continue;
-        // (a loop that is not taken apart would have the logits in memory)
-        _Pragma("unroll") for (int c = 0; c < 16; ++c) {
-            const double e = top == -NINF ? (x[c] == top ? 1.0 : 0.0) : exp_of((double)x[c] - (double)top);
-            sum += ((counted >> c) & 1u) && x[c] > NINF ? e : 0.0;
+        if (infinite) { _Pragma("unroll") for (int c = 0; c < 16; ++c) x[c] = x[c] == -NINF ? 0.f : NINF; }
+        _Pragma("unroll") for (int c = 0; c < 16; c += 4) {
+            double d[4];
+            _Pragma("unroll") for (int i = 0; i < 4; ++i) {
+                // (a bit spread over a word picks the logit or minus infinity; the larger of NaN and a number is the number)
+                const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)counted, c + i, 1);
+                const float y = larger(x[c + i], NINF);
+                d[i] = (double)__uint_as_float((__float_as_uint(y) & m) | (__float_as_uint(NINF) & ~m)) - from;
+            }
+            sum += sum_of_exps(d);
         }
     }
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
@@ -467,8 +490,8 @@ __device__ __attribute__((noinline)) void repair_row(PickArgs args, PickLds lds,
         S.exact[k] = 1;
         if (top == NINF) S.state[k] = ROW_NONE;
         else {
-            S.infinite[k] = top == -NINF;
-            S.base[k] = (double)score - (log(all) + (top == -NINF ? 0.0 : (double)top));
+            S.infinite[k] = infinite;
+            S.base[k] = (double)score - (log(all) + from);
         }
     }
     __threadfence_block();
