@@ -137,6 +137,48 @@ def test_slots_with_deep_contexts_and_errors(xg):
         assert np.array_equal(got[b], oracle.pack_bitmask(orc.mask(b"x" * x, va))), b
 
 
+def test_slots_of_different_grammars_in_a_group(xg):
+    """A slot takes over its parent's grammar with its state, and keeps it; a slot that is reset meanwhile starts again with another."""
+    import torch
+    cfg, vocab, va = load(1)
+    grammars = [cfg.grammars[0], ('root ::= "[" ws (num (ws "," ws num)*)? ws "]"\nnum ::= "-"? [0-9]{1,4}\nws ::= [ \t\n]*\n', "root"),
+                ('root ::= item+\nitem ::= "<" [a-z]{1,8} ">" | [A-Z ]\n', "root")]
+    caches = [xg.compile_grammar(vocab, e, r, stream=_stream()) for e, r in grammars]
+    orcs = [oracle.Oracle(e, r) for e, r in grammars]
+    G, K = 3, 7
+    B = G * K
+    rng, pick = np.random.default_rng(5), random.Random(5)
+    db = xg.DeviceBatch(vocab, B)
+    state = [(b % 3, b"") for b in range(B)]
+    for b in range(B):
+        db.assign(caches[b % 3], rows=[b], stream=_stream())
+    status = torch.zeros(B, dtype=torch.int32, device="cuda")
+    bitmask = torch.zeros((B, vocab.words), dtype=torch.int32, device="cuda")
+    for step in range(8):
+        parents = _parents(rng, G, K)
+        p = torch.from_numpy(parents).cuda()
+        db.reorder(K, p.data_ptr(), p.data_ptr(), _stream())         # (the statuses may take the parents' place)
+        assert not p.cpu().numpy().any()
+        state = ref.reorder(state, parents, G, K)
+        if step == 4:
+            for b in (0, 8, 20):
+                db.assign(caches[(b + 1) % 3], rows=[b], stream=_stream())
+                state[b] = ((b + 1) % 3, b"")
+        db.fill_next_token_bitmask(bitmask.data_ptr(), vocab.words, _stream())
+        got = bitmask.cpu().numpy()
+        nxt = np.full(B, -1, dtype=np.int32)
+        for b, (c, h) in enumerate(state):
+            want = orcs[c].mask(h, va)
+            assert np.array_equal(got[b], oracle.pack_bitmask(want)), (step, b)
+            can = [t for t in np.flatnonzero(want).tolist() if t != cfg.vocab.eos_id]
+            if can and pick.random() < 0.9:
+                nxt[b] = pick.choice(can)
+                state[b] = (c, h + cfg.vocab.tokens[nxt[b]])
+        ids = torch.from_numpy(nxt).cuda()
+        db.accept_tokens(ids.data_ptr(), status.data_ptr(), _stream())
+        assert not status.cpu().numpy().any()
+
+
 def test_slots_refusals(xg):
     import torch
     cfg, vocab, _ = load(1)
@@ -213,6 +255,15 @@ def test_rows_permutations_and_cycles(xg):
                                      piece_stride=40 * 96, stream=_stream())
                 x = x[:, q.long()]
             assert torch.equal(d, x), (K, name)
+
+
+def test_rows_of_many_groups_and_pieces(xg):
+    """More groups than one dimension of a grid takes; rows of very many small pieces; one long piece."""
+    rng = np.random.default_rng(31)
+    _rows_case(xg, rng, 33003, 2, 1, 2, 3, 5, "heads", "both", 0)
+    _rows_case(xg, rng, 2, 3, 3, 200_003, 2, 3, "heads", "both", 1)
+    _rows_case(xg, rng, 1, 5, 1, 1, 1_000_003, 7, "heads", "both", 3)
+    _rows_case(xg, rng, 1, 40, 1, 1, 100_003, 7, "heads", "none", 2)
 
 
 def test_rows_beyond_4_gib(xg):

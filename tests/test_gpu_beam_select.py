@@ -260,6 +260,62 @@ def test_large_vocabulary_and_many_rows(xg):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_nearly_the_same(xg, dtype):
+    """All tokens as far from their beams as the others: from logits that differ by tenths to those that differ in their last bits."""
+    rng = np.random.default_rng(21)
+    for k, (G, K, V, n) in enumerate([(1, 4, 9000, 8), (2, 16, 20011, 64), (1, 64, 3001, 128), (3, 2, 50021, 1)]):
+        for spread, level in ((0.3, 0.0), (0.03, 0.0), (1e-3, 5.0), (1e-5, -2.0)):
+            x = (rng.standard_normal((G * K, V)) * spread + level).astype(np.float32)
+            scores = -rng.random(G * K) * (4 * spread if k % 2 else 2.0) - 1
+            finished = (rng.random(G * K) < 0.1).astype(np.int32)
+            allowed = rng.random((G * K, V)) < 0.9 if k % 2 else None
+            Call(xg, x, allowed, scores, finished, G, K, n, bool(k & 2), dtype).check((G, K, V, n, spread))
+
+
+def test_one_workspace_for_calls_in_a_row(xg):
+    """Calls of other sizes, types and masks, one behind the other in a stream, take turns in one workspace."""
+    import torch
+    rng = np.random.default_rng(22)
+    calls = [Call(xg, *_inputs(rng, G, K, V, mask), G, K, n, over, dtype, pad=5)
+             for G, K, V, n, mask, over, dtype in ((4, 8, 30011, 16, "mixed", False, "bf16"), (1, 3, 500, 4, "empty", False, "f32"), (2, 32, 7000, 64, "few", True, "f32"), (9, 5, 2100, 9, "none", True, "bf16"))]
+    work = torch.full((max(c.size for c in calls) + 64,), 0x5A, dtype=torch.uint8, device="cuda")
+    for c in calls:
+        c.work = work
+    for _ in range(3):
+        for c in calls:
+            c.run()
+    biggest = max(c.size for c in calls)
+    for c in calls:
+        c.size = biggest                                             # (what lies behind a smaller call's part belongs to the others)
+        got = c.outputs()
+        want = ref.select(c.x, c.allowed, c.scores, c.finished, c.G, c.K, c.n, c.over_all, c.eos)
+        assert all(np.array_equal(g, w) for g, w in zip(got[1:], want[1:]))
+
+
+def test_logits_and_masks_beyond_4_gib(xg):
+    """Rows 3 GB apart, their masks 1.4 GB apart."""
+    import torch
+    K, V, stride, words = 3, 5003, 1_500_000_019, 350_000_000
+    rng = np.random.default_rng(23)
+    x = ref.to_bf16((rng.standard_normal((K, V)) * 2).astype(np.float32))
+    allowed = rng.random((K, V)) < 0.5
+    scores = np.array([-1.0, -1.5, -0.5], dtype=np.float32)
+    logits, mask = torch.empty(2 * stride + V, dtype=torch.int16, device="cuda"), torch.empty(2 * words + (V + 31) // 32, dtype=torch.int32, device="cuda")
+    for k in range(K):
+        logits[k * stride:k * stride + V] = _put(x[k].view(np.int16))
+        mask[k * words:k * words + (V + 31) // 32] = _put(oracle.pack_bitmask(allowed[k]))
+    n = 40
+    o = [torch.empty(n, dtype=t, device="cuda") for t in (torch.float32, torch.int32, torch.int32, torch.int32)]
+    d_scores = _put(scores)
+    work = torch.empty(xg.beam_select_workspace(xg.XG2_BF16, 1, K, V, n), dtype=torch.uint8, device="cuda")
+    xg.beam_select(logits.data_ptr(), xg.XG2_BF16, 1, K, V, stride, d_scores.data_ptr(), n, o[0].data_ptr(), o[1].data_ptr(), o[2].data_ptr(), work.data_ptr(), work.numel(),
+                   bitmask_ptr=mask.data_ptr(), bm_row_stride_words=words, eos_id=0, out_finished_ptr=o[3].data_ptr(), stream=_stream())
+    want = ref.select(ref.from_bf16(x), allowed, scores, None, 1, K, n, False, 0)
+    assert all(np.array_equal(g.cpu().numpy().reshape(1, n), w) for g, w in zip(o[1:], want[1:]))
+    assert (np.abs(o[0].cpu().numpy() - want[0][0]) <= ref.score_tolerance(V, want[0][0])).all()
+
+
 def test_calls_at_the_same_time(xg):
     """Two calls on two streams, each with its own workspace, and the same call again: every result the same."""
     import torch
