@@ -76,11 +76,13 @@ __device__ __forceinline__ float sum_of_64(float v) {                           
 //
 // The pass: a wavefront per piece, counted from the 128-byte boundary at or before the row's begin, so that all vectors are aligned
 // whatever the row; 32 logits a lane in registers, all loaded before the first is used; under a mask one word of it a lane, vectors
-// without an allowed token not loaded and pieces without one not looked at.  The piece's maximum goes into the exponents as it is (no
+// without an allowed token not loaded and pieces without one not looked at; where no mask word allows more than six tokens, each lane loads
+// those of its word alone (4 rows of 32,000 tokens with two dozen allowed, us with the second kernel: vectors 10.6, up to three 10.1, up to
+// six 9.6).  The piece's maximum goes into the exponents as it is (no
 // running maximum, no second exponential).  Bound by memory and, over bfloat16, as much by instructions (8.5 a logit, one of them at a
 // quarter rate: 47 us of issue and 46 us of memory for 1,024 rows of V = 151,936, 311 MB of logits and 19 of masks, which take 47.5 us,
-// 6.9 TB/s).  256 rows fp32, masks of all kinds 14.4 us; 64 rows of V = 128,256 4.1; 4 rows of 32,000 with few tokens allowed 4.0.
-constexpr int kScanWaves = 4;
+// 6.9 TB/s).  256 rows fp32, masks of all kinds 14.4 us; 64 rows of V = 128,256 4.1; 4 rows of 32,000 with few tokens allowed 3.1.
+constexpr int kScanWaves = 4, kScanFew = 6;
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr double LN2 = 0.693147180559945309417232;
 
@@ -159,6 +161,26 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
     if (WHICH == 1 && __ballot(counted != 0) == 0) {
         if (lane == 0) *stats = stats_of(NINF, 0.f, NINF);
         if (lane < kBeamPieceBlocks) block_max[lane] = NINF;                           // (a wavefront has as many lanes)
+        return;
+    }
+    if (WHICH == 1 && __ballot(__popc(counted) > kScanFew) == 0) {
+        // few tokens: each lane takes its own one by one, two lanes have a block (5 and 6 additions between a term and the sum)
+        float x[kScanFew], own = NINF;
+        uint32_t left = counted;
+        _Pragma("unroll") for (int c = 0; c < kScanFew; ++c, left &= left - 1) {
+            x[c] = NINF;
+            if (left != 0) x[c] = Elem<E>::load(row + (first + __ffs((int)left) - 1));
+        }
+        _Pragma("unroll") for (int c = 0; c < kScanFew; ++c) own = fmaxf(own, x[c]);
+        const float block = fmaxf(own, moved<DPP_SWAP1>(own, own)), all = lane_float(largest_of_64(own), 63);
+        if (lane % 2 == 0) block_max[lane / 2] = block;
+        float sum = 0;
+        if (all > NINF) {
+            const float c = larger(__fmul_rn(all, LOG2E), -3.4028234e38f);
+            _Pragma("unroll") for (int i = 0; i < kScanFew; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], LOG2E, -c));
+            sum = sum_of_64(sum);
+        }
+        if (lane == 63) *stats = stats_of(all, sum, all);
         return;
     }
     const E* const from = row + e0;

@@ -273,6 +273,29 @@ def test_logits_nearly_the_same(xg, dtype):
             Call(xg, x, allowed, scores, finished, G, K, n, bool(k & 2), dtype).check((G, K, V, n, spread))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_masks_of_few_tokens_a_word(xg, dtype):
+    """Words that allow one, six and seven tokens, at a row's ends too; NaN and infinities among them and beside them."""
+    rng = np.random.default_rng(24)
+    for V in (31, 200, 2048, 5003):
+        for most in (1, 3, 6, 7):
+            x = (rng.standard_normal((6, V)) * 2).astype(np.float32)
+            allowed = np.zeros((6, V), dtype=bool)
+            for r in range(6):
+                for w in range(0, V, 32):
+                    n = min(32, V - w)
+                    allowed[r, w + rng.choice(n, min(n, most if rng.random() < 0.3 else rng.integers(0, most + 1)), replace=False)] = True
+            allowed[0, [0, V - 1]] = True
+            odd = rng.random((6, V)) < 0.05
+            x[odd] = rng.choice(np.array([np.nan, -np.inf], dtype=np.float32), odd.sum())
+            x[3] = np.where(allowed[3], np.nan, x[3])                # (nothing but NaN)
+            x[4, np.flatnonzero(allowed[4])[:2]] = np.inf
+            x[5] = np.where(allowed[5], x[5], np.nan)
+            scores = -rng.random(6) - 1
+            for K, offset in ((1, 0), (3, 1), (6, 3)):
+                Call(xg, x, allowed, scores, None, 6 // K, K, 10, False, dtype, offset=offset, pad=7).check((V, most, K))
+
+
 def test_one_workspace_for_calls_in_a_row(xg):
     """Calls of other sizes, types and masks, one behind the other in a stream, take turns in one workspace."""
     import torch
