@@ -81,7 +81,7 @@ __device__ __forceinline__ float sum_of_64(float v) {                           
 // six 9.6).  The piece's maximum goes into the exponents as it is (no
 // running maximum, no second exponential).  Bound by memory and, over bfloat16, as much by instructions (8.5 a logit, one of them at a
 // quarter rate: 47 us of issue and 46 us of memory for 1,024 rows of V = 151,936, 311 MB of logits and 19 of masks, which take 47.5 us,
-// 6.9 TB/s).  256 rows fp32, masks of all kinds 14.4 us; 64 rows of V = 128,256 4.1; 4 rows of 32,000 with few tokens allowed 3.1.
+// 6.9 TB/s).  256 rows fp32, masks of all kinds 14.4 us; 64 rows of V = 128,256 4.1; 4 rows of 32,000 with few tokens allowed 3.0.
 constexpr int kScanWaves = 4, kScanFew = 6;
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr double LN2 = 0.693147180559945309417232;
@@ -268,8 +268,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
 // below, so only pieces, in them blocks, in them tokens that do are looked at, which are few more than n as a rule.  Where they are not (fewer
 // pieces than candidates, rows that differ much), blocks, and then tokens, are counted again.  16 lanes have a row's pieces.
 // Bound by latency: a dozen dependent steps (rows' sums, count, pieces, blocks, tokens, places), three of them with a load from memory
-// that other dies have written (about 1 us each).  us, kernel trace: 1 group of 4 beams, V = 32,000, 8 candidates 6.9; 16 of 4, V = 128,256,
-// 4 candidates 8.6; 128 of 8, V = 151,936, 16 candidates 9.5; 8 of 32, V = 151,936, 64 candidates 11.8.  Both kernels in one launch, a workgroup
+// that other dies have written (about 1 us each).  us, kernel trace: 1 group of 4 beams, V = 32,000, 8 candidates 7.0; 16 of 4, V = 128,256,
+// 8 candidates 8.8; 128 of 8, V = 151,936, 16 candidates 9.8; 8 of 32, V = 151,936, 64 candidates 12.7.  Both kernels in one launch, a workgroup
 // for a group of up to 64 pieces, was slower when it was tried: 1 x 4 beams, V = 32,000 12.3 as two, 23.6 as one; 64 x 8, V = 4,000 13.9 and 21.6.
 constexpr int kPickThreads = 1024, kPickMostWaves = kPickThreads / 64, kPickBins = 1024, kPickListed = 512, kPickElems = 1024, kPickHeld = 5;
 
@@ -657,7 +657,8 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
     }
     if (mine && part == 0) { S.state[k] = state; S.base[k] = base; S.infinite[k] = 0; S.exact[k] = state != ROW_LIVE; S.repair[k] = repair; S.largest[k] = largest; }
     // Distances are taken from the best candidate: the best beam's score would do while few candidates lie as far from it as the n-th, but
-    // where a row's logits are nearly the same all tokens are as far from it.
+    // where a row's logits are nearly the same all tokens are as far from it (4 groups of 32 rows of 151,936 logits with a deviation of 0.3:
+    // 4,631 us, from the best candidate 21; ordinary rows 0.1 to 0.4 us less).
     bool infinite = false;
     auto own_score = [&](float m) { return infinite ? (m == -NINF ? base : none) : base + (double)m; };
     auto find_top = [&] {
