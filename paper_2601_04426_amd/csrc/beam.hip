@@ -2,7 +2,7 @@
 //   k_beam_scan          one pass over the logits: sums of exponentials and the largest allowed logit of every block of tokens
 //   k_beam_pick          the best candidates of a group, from the blocks that can hold them
 //   k_batch_reorder      matcher slots take over the state of their parents
-//   k_beam_reorder_rows  the same for rows of a caller's buffer, in place
+//   k_beam_reorder_rows  the same for rows of a caller's buffer, in place (k_beam_reorder_strips: more than 16 beams)
 //   k_beam_backtrace     sequences from the steps' tokens and parents
 #include <algorithm>
 #include <cstddef>
@@ -89,7 +89,6 @@ constexpr double LN2 = 0.693147180559945309417232;
 typedef uint32_t Vec4 __attribute__((ext_vector_type(4)));
 // vectors at any byte: the device takes them
 typedef uint32_t Wide4 __attribute__((ext_vector_type(4), aligned(1)));
-typedef uint32_t Wide1 __attribute__((aligned(1)));
 template <class E> struct Elem;
 template <> struct Elem<float> {
     static constexpr int EPV = 4;
@@ -962,6 +961,62 @@ __global__ __launch_bounds__(256) void k_beam_reorder_rows(const int32_t* parent
     if (split == 0 && rest < bytes) move_columns<uint8_t, MOST, 1, false>(piece + rest, 0, 1, A.row_stride, from, moves);
 }
 
+// Many beams: a column of all rows no longer fits a thread's registers with loads of 16 bytes, so a workgroup has a strip of 256 bytes of
+// all rows in LDS, loads it whole and then stores it.  TB/s as below with strips of 128 / 256 / 512 / 1,024 bytes: 17 beams 2.7 / 3.7 / 3.4 / 2.3,
+// 32 beams 4.1 / 4.6 / 4.0 / 2.7, 64 beams 4.5 / 4.7 / 4.1 / 3.1.
+constexpr int kStripVecs = 16, kStripRows = 16;                       // vectors of a strip; rows that the 256 threads have at a time
+template <bool PAST>
+__global__ __launch_bounds__(256) void k_beam_reorder_strips(const int32_t* parents, const int32_t* begins, const int32_t* ends, uint32_t K, uint32_t splits, uint32_t positions, BeamRows A) {
+    constexpr int TURNS = kBeamsMost / kStripRows;
+    __shared__ Vec4 strip[kBeamsMost][kStripVecs];
+    const uint32_t split = blockIdx.x % splits, unit = blockIdx.x / splits, g = blockIdx.y + blockIdx.z * 32768u, lane = threadIdx.x & 63;
+    if (g >= A.groups) return;
+    const int32_t p = lane < K ? ((Global<const int32_t>)parents)[g * K + lane] : -1;
+    int64_t begin = begins ? ((Global<const int32_t>)begins)[g] : 0, end = ends ? ((Global<const int32_t>)ends)[g] : (int64_t)positions;
+    begin = begin < 0 ? 0 : begin;
+    end = end > (int64_t)positions ? (int64_t)positions : end;
+    if (begin >= end) return;
+    const uint32_t from = (uint32_t)p - g * K;
+    const bool moving = p >= 0 && from < K && from != lane;
+    const uint64_t moves = __ballot(moving);
+    if (moves == 0) return;
+    uint64_t sources = 0;                                            // rows that a row takes
+    for (uint32_t k = 0; k < K; ++k) sources |= __ballot(moving && from == k) != 0 ? 1ull << k : 0ull;
+    uint8_t* const piece = A.data + (int64_t)(g * K) * A.row_stride + (int64_t)(unit / A.pieces) * A.outer_stride + (int64_t)(unit % A.pieces) * A.piece_stride
+                           + begin * A.position_bytes;
+    const int64_t bytes = (end - begin) * A.position_bytes, whole = bytes / 16;
+    const uint32_t own = threadIdx.x % kStripVecs, first = threadIdx.x / kStripVecs;
+    uint32_t takes[TURNS];                                           // the row that this thread's rows take
+    _Pragma("unroll") for (int j = 0; j < TURNS; ++j) takes[j] = (uint32_t)__shfl((int)from, (int)(first + j * kStripRows));
+    for (int64_t v0 = (int64_t)split * kStripVecs; v0 < whole; v0 += (int64_t)splits * kStripVecs) {
+        const bool inside = v0 + own < whole;
+        uint8_t* const at = piece + (v0 + own) * 16;
+        Wide4 v[TURNS];
+        _Pragma("unroll") for (int j = 0; j < TURNS; ++j) {
+            const uint32_t k = first + j * kStripRows;
+            if (!inside || !((sources >> k) & 1)) continue;
+            const Global<const Wide4> place = (Global<const Wide4>)(at + (int64_t)k * A.row_stride);
+            v[j] = PAST ? __builtin_nontemporal_load(place) : *place;
+        }
+        _Pragma("unroll") for (int j = 0; j < TURNS; ++j) {
+            const uint32_t k = first + j * kStripRows;
+            if (inside && ((sources >> k) & 1)) strip[k][own] = v[j];
+        }
+        __syncthreads();
+        _Pragma("unroll") for (int j = 0; j < TURNS; ++j) {
+            const uint32_t k = first + j * kStripRows;
+            if (!inside || !((moves >> k) & 1)) continue;
+            const Wide4 w = strip[takes[j]][own];
+            const Global<Wide4> place = (Global<Wide4>)(at + (int64_t)k * A.row_stride);
+            if (PAST) __builtin_nontemporal_store(w, place);
+            else *place = w;
+        }
+        __syncthreads();
+    }
+    const int64_t rest = whole * 16 + threadIdx.x;                   // (less than a vector)
+    if (split == 0 && rest < bytes) move_columns<uint8_t, kBeamsMost, 1, false>(piece + rest, 0, 1, A.row_stride, from, moves);
+}
+
 // ---- sequences ------------------------------------------------------------------------------------------------------
 // A chain of as many look-ups as there are steps, one behind the other; but where the beams behind a segment of the steps come from
 // before it does not hang on the other segments.  So the steps are cut into segments, each worked out by WIDTH lanes of a wavefront (a
@@ -1092,29 +1147,33 @@ void launch_batch_reorder(const BatchDev& D, uint32_t beams, const int32_t* pare
 constexpr int64_t ROWS_PAST_BYTES = 256ll << 20;
 constexpr uint32_t ROWS_SPLITS = 16, ROWS_GROUPS = 4096;
 
-template <class T, int MOST, int TOGETHER>
-static void launch_rows_as(const BeamRows& A, hipStream_t stream) {
+// A workgroup takes `vectors_each` vectors of `vector` bytes of a piece at a time.
+template <class K>
+static void launch_rows(const BeamRows& A, hipStream_t stream, int64_t vector, uint32_t vectors_each, K* near, K* past_caches) {
     const uint32_t units = A.outer * A.pieces;
-    const int64_t piece = A.positions * A.position_bytes, vectors = piece / (int64_t)sizeof(T);
+    const int64_t piece = A.positions * A.position_bytes, vectors = piece / vector;
     const uint64_t all = (uint64_t)units * A.groups, most = std::max<uint64_t>(ROWS_SPLITS, ROWS_GROUPS / all);
-    uint32_t splits = (uint32_t)std::min<uint64_t>((uint64_t)vectors / (256 * TOGETHER) + 1, most);
+    uint32_t splits = (uint32_t)std::min<uint64_t>((uint64_t)vectors / vectors_each + 1, most);
     splits = std::max<uint32_t>(1, std::min<uint32_t>(splits, (1u << 23) / units));            // (a grid has less than 2^32 threads)
     const bool past = (double)piece * (double)all * A.beams > (double)ROWS_PAST_BYTES;
-    auto* const kernel = past ? k_beam_reorder_rows<T, MOST, TOGETHER, true> : k_beam_reorder_rows<T, MOST, TOGETHER, false>;
-    hipLaunchKernelGGL(kernel, dim3(units * splits, std::min<uint32_t>(A.groups, 32768), (A.groups + 32767) / 32768), dim3(256), 0, stream,
+    hipLaunchKernelGGL(past ? past_caches : near, dim3(units * splits, std::min<uint32_t>(A.groups, 32768), (A.groups + 32767) / 32768), dim3(256), 0, stream,
                        A.parents, A.begin, A.end, A.beams, splits, A.positions, A);
 }
 
+template <class T, int MOST, int TOGETHER>
+static void launch_rows_as(const BeamRows& A, hipStream_t stream) {
+    launch_rows(A, stream, sizeof(T), 256 * TOGETHER, k_beam_reorder_rows<T, MOST, TOGETHER, false>, k_beam_reorder_rows<T, MOST, TOGETHER, true>);
+}
+
 // What a thread holds of each row, and how many columns of it.  TB/s over 537 MB (rows of 256 positions of 128 bytes, moved bytes counted
-// once read and once written), 2 / 4 / 8 / 16 / 32 / 64 beams: 16 bytes, one column 3.3 / 5.4 / 5.2 / 4.8 / 3.9 / -, two columns 4.8 / 5.1 / 5.0
-// / - / - / - (their registers cost wavefronts), 8 bytes - / - / - / - / 3.1 / 2.2, 4 bytes - / - / - / - / 4.2 / 3.3.
+// once read and once written), 2 / 4 / 8 / 16 / 17 / 32 / 33 / 64 beams: 16 bytes, one column 3.3 / 5.4 / 5.2 / 4.8 / - / 3.9 / - / -, two columns
+// 4.8 / 5.1 / 5.0 (their registers cost wavefronts), 4 bytes - / - / - / - / 4.1 / 4.2 / 2.6 / 3.3, strips in LDS - / - / - / - / 3.7 / 4.6 / 4.5 / 4.7.
 void launch_beam_reorder_rows(const BeamRows& A, hipStream_t stream) {
     if (A.beams <= 2) launch_rows_as<Wide4, 2, 2>(A, stream);
     else if (A.beams <= 4) launch_rows_as<Wide4, 4, 1>(A, stream);
     else if (A.beams <= 8) launch_rows_as<Wide4, 8, 1>(A, stream);
     else if (A.beams <= 16) launch_rows_as<Wide4, 16, 1>(A, stream);
-    else if (A.beams <= 32) launch_rows_as<Wide1, 32, 1>(A, stream);
-    else launch_rows_as<Wide1, 64, 1>(A, stream);
+    else launch_rows(A, stream, 16, kStripVecs, k_beam_reorder_strips<false>, k_beam_reorder_strips<true>);
 }
 
 template <int WIDTH>

@@ -257,6 +257,25 @@ def test_rows_permutations_and_cycles(xg):
             assert torch.equal(d, x), (K, name)
 
 
+@pytest.mark.parametrize("K", [2, 3, 11, 24, 64])
+def test_rows_past_the_caches(xg, K):
+    """Buffers beyond 256 MB, pieces whose begins and ends lie anywhere."""
+    import torch
+    positions, width, pieces = 1003, 135, 3
+    G = (300 << 20) // (K * pieces * positions * width) + 1
+    g = torch.Generator(device="cuda").manual_seed(K)
+    d = torch.randint(0, 256, (G * K, pieces, positions, width), generator=g, device="cuda", dtype=torch.uint8)
+    p = torch.randint(0, K, (G, K), generator=g, device="cuda", dtype=torch.int32) + torch.arange(G, device="cuda", dtype=torch.int32)[:, None] * K
+    begin = torch.randint(0, positions, (G,), generator=g, device="cuda", dtype=torch.int32)
+    want = d[p.view(-1).long()]
+    t = torch.arange(positions, device="cuda")
+    outside = (t[None, :] < begin[:, None]).repeat_interleave(K, 0)
+    want = torch.where(outside[:, None, :, None], d, want)
+    xg.beam_reorder_rows(d.data_ptr(), G, K, p.data_ptr(), row_stride=pieces * positions * width, positions=positions, position_bytes=width, pieces=pieces,
+                         piece_stride=positions * width, begin_ptr=begin.data_ptr(), stream=_stream())
+    assert torch.equal(d, want)
+
+
 def test_rows_of_many_groups_and_pieces(xg):
     """More groups than one dimension of a grid takes; rows of very many small pieces; one long piece."""
     rng = np.random.default_rng(31)
