@@ -31,8 +31,8 @@ __device__ __forceinline__ float lane_float(float v, int lane) { return __int_as
 constexpr int DPP_SWAP1 = 0xB1, DPP_SWAP2 = 0x4E, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140, DPP_ROW_BCAST15 = 0x142, DPP_ROW_BCAST31 = 0x143;
 template <int CTRL, int ROWS = 0xF>
 __device__ __forceinline__ float moved(float own, float v) { return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(own), __float_as_int(v), CTRL, ROWS, 0xF, false)); }
-// The larger of two (three) numbers, of two with a quiet NaN the other.  (fmaxf would take an instruction more for each operand that came
-// from memory, to make signalling NaN quiet ones; where one of these is met the sum of exponentials is NaN, which is looked for.)
+// The larger of two (three) numbers, of two with a quiet NaN the other.  A signalling NaN takes the number away, in v_max_f32 and in what the
+// compiler makes of fmaxf, so who takes the maximum of values from memory looks for NaN among them.
 __device__ __forceinline__ float larger(float a, float b) { float d; asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b)); return d; }
 __device__ __forceinline__ float larger(float a, float b, float c) { float d; asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c)); return d; }
 // Four values at a time, stage by stage, so that none is read across lanes within two instructions of being written (which the device does
@@ -114,6 +114,21 @@ template <> struct Elem<uint16_t> {                                  // bfloat16
     }
 };
 
+// Whether a lane has a signalling NaN among its values.  A piece's sum is NaN if a term is, whereupon the choice looks through the row again;
+// where no maximum is left to take a sum of, what counts may have fallen to a signalling NaN, and the sum has to say so too.
+template <int N>
+__device__ __forceinline__ bool signalling(const float (&x)[N]) {
+    bool any = false;
+    _Pragma("unroll") for (int i = 0; i < N; ++i) any |= __builtin_amdgcn_classf(x[i], 1);
+    return any;
+}
+template <int M, int N>
+__device__ __forceinline__ bool signalling(const float (&x)[M][N]) {
+    bool any = false;
+    _Pragma("unroll") for (int i = 0; i < M; ++i) any |= signalling(x[i]);
+    return any;
+}
+
 __device__ __forceinline__ Vec4 stats_of(float top, float sum, float best) { return Vec4{__float_as_uint(top), __float_as_uint(sum), __float_as_uint(best), 0u}; }
 
 // Elements of a row before the 128-byte boundary that its pieces and blocks are counted from.
@@ -178,7 +193,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
             const float c = larger(__fmul_rn(all, LOG2E), -3.4028234e38f);
             _Pragma("unroll") for (int i = 0; i < kScanFew; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], LOG2E, -c));
             sum = sum_of_64(sum);
-        }
+        } else if (__ballot(signalling(x)) != 0) sum = __builtin_nanf("");
         if (lane == 63) *stats = stats_of(all, sum, all);
         return;
     }
@@ -257,7 +272,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
         _Pragma("unroll") for (int d = STEPS * EPV / 2; d > 0; d /= 2)
             _Pragma("unroll") for (int i = 0; i < d; ++i) part[i] += part[i + d];
         sum = sum_of_64(part[0]);
-    }
+    } else if (__ballot(signalling(x)) != 0) sum = __builtin_nanf("");
     if (lane == 63) *stats = stats_of(all, sum, ok_max);
 }
 
@@ -494,10 +509,9 @@ __device__ __attribute__((noinline)) void repair_row(PickArgs args, PickLds lds,
         _Pragma("unroll") for (int c = 0; c < 16; c += 4) {
             double d[4];
             _Pragma("unroll") for (int i = 0; i < 4; ++i) {
-                // (a bit spread over a word picks the logit or minus infinity; the larger of NaN and a number is the number)
+                // (a bit spread over a word picks the logit or minus infinity; what is NaN counts nothing, sum_of_exps sees to it)
                 const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)counted, c + i, 1);
-                const float y = larger(x[c + i], NINF);
-                d[i] = (double)__uint_as_float((__float_as_uint(y) & m) | (__float_as_uint(NINF) & ~m)) - from;
+                d[i] = (double)__uint_as_float((__float_as_uint(x[c + i]) & m) | (__float_as_uint(NINF) & ~m)) - from;
             }
             sum += sum_of_exps(d);
         }
