@@ -787,9 +787,10 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
             Sixteen<E> T;
             T.ask(A, row_r, t0, false);
             const uint32_t ok = T.take(A.V, t0, x);
-            // a bound in 32 bits first
-            const double least = reach - S.base[row_k];
-            const float bound = (float)least - (__builtin_fabsf((float)least) * 1e-6f + 1e-3f);
+            // a bound in 32 bits first, below what is sought by more than its own rounding (1e-6 of it) and that of the three sums in 64
+            // bits behind it (half a place each, 2^-53 of a base that can be 1e14 times a logit: tokens that differ have one score then)
+            const double base = S.base[row_k], least = reach - base;
+            const float bound = (float)least - (__builtin_fabsf((float)least) * 1e-6f + 1e-3f + (float)__builtin_fabs(base) * 0x1p-50f);
             uint32_t hits = 0;
             _Pragma("unroll") for (int c = 0; c < 16; ++c) hits |= x[c] >= bound ? 1u << c : 0u;
             for (hits &= ok; hits != 0; hits &= hits - 1) {
