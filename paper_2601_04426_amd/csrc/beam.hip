@@ -6,6 +6,7 @@
 //   k_beam_backtrace     sequences from the steps' tokens and parents
 #include <algorithm>
 #include <cstddef>
+#include <type_traits>
 
 #include "beam.hpp"
 
@@ -434,10 +435,11 @@ struct Sixteen {
 #endif
 typedef const XG2_CONSTANT BeamSelect* PickArgs;
 typedef XG2_LDS PickShared* PickLds;
-static_assert(alignof(BeamSelect) == 8, "k_beam_pick's struct of arguments lies 40 bytes on, behind three pointers and three words");
+// k_beam_pick's arguments as they lie in memory, one behind the other at its type's alignment; the kernel's type is held against it below.
+struct PickParams { const float4* all_stats; const float* scores; const int32_t* finished; uint32_t K, pieces, N; BeamSelect A; };
 __device__ __forceinline__ PickArgs pick_args() {
 #if defined(__HIP_DEVICE_COMPILE__)
-    return (PickArgs)((const XG2_CONSTANT char*)__builtin_amdgcn_kernarg_segment_ptr() + 40);
+    return (PickArgs)((const XG2_CONSTANT char*)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(PickParams, A));
 #else
     return nullptr;
 #endif
@@ -853,6 +855,11 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
     }
     if (tid < N) write_choice(A, g, tid, tid < R, tid < R ? S.found[S.sorted[tid]] : Candidate{0, 0});
 }
+
+template <class... P> using Kernel = void(P...);
+static_assert(std::is_same_v<decltype(k_beam_pick<float>), Kernel<decltype(PickParams::all_stats), decltype(PickParams::scores), decltype(PickParams::finished), decltype(PickParams::K),
+                                                                  decltype(PickParams::pieces), decltype(PickParams::N), decltype(PickParams::A)>> &&
+              std::is_standard_layout_v<PickParams>, "k_beam_pick finds its last argument at its place in PickParams");
 
 // ---- matcher slots --------------------------------------------------------------------------------------------------
 // One workgroup per group of beams, a wavefront for up to SLOTS of its slots.  A slot's context has two buffers, and nobody reads the one
