@@ -319,10 +319,12 @@ int32_t xg2_apply_token_bitmask(void* logits_dev, int32_t dtype, int32_t B, int3
  * over = XG2_OVER_ALLOWED: the allowed tokens of the row count (probabilities given that the grammar is kept to);
  * XG2_OVER_ALL: all V tokens count (the model's own probabilities).  A beam that has ended (finished[row] != 0; finished_dev
  * may be NULL) is one candidate: its score as it is, with token -1.  Chosen are the largest scores, among equal ones the lowest
- * row, in it the lowest token.  Scores are compared as sums in 64 bits give them.
+ * row, in it the lowest token.  Scores are compared as sums in 64 bits give them (of the same terms in another order a sum may differ
+ * in its last place, and so may the scores of two rows that hold the same logits at other tokens).
  *   logits_dev: G * K rows of row_stride_elems elements (XG2_F32 or XG2_BF16), at a multiple of the element's size; not written.
  *   bitmask_dev: rows of bm_row_stride_words words as xg2_batch_fill_next_token_bitmask writes them, or NULL: all are allowed.
- *   scores_dev: float32 per row; -infinity (also +infinity and NaN): no beam, the row is not read.
+ *   scores_dev: float32 per row; -infinity (also +infinity and NaN): no beam, the row is not read.  A search begins with one beam and
+ *   the others at -infinity; a large finite score in its place (beyond 1e6 in size) is taken as it is, at the cost of a sum in 64 bits.
  * A row that allows nothing has no candidates.  A logit of NaN or -infinity is no candidate and does not count; where
  * +infinity counts, the tokens that have it share the probability evenly and the others have none.
  * Out, [G, n_out] each, best first: scores, parents (rows), tokens, and (may be NULL) whether the continuation has ended:

@@ -81,8 +81,8 @@ __device__ __forceinline__ float sum_of_64(float v) {                           
 // those of its word alone (4 rows of 32,000 tokens with two dozen allowed, us with the second kernel: vectors 10.6, up to three 10.1, up to
 // six 9.6).  The piece's maximum goes into the exponents as it is (no
 // running maximum, no second exponential).  Bound by memory and, over bfloat16, as much by instructions (8.5 a logit, one of them at a
-// quarter rate: 47 us of issue and 46 us of memory for 1,024 rows of V = 151,936, 311 MB of logits and 19 of masks, which take 47.5 us,
-// 6.9 TB/s).  256 rows fp32, masks of all kinds 14.4 us; 64 rows of V = 128,256 4.1; 4 rows of 32,000 with few tokens allowed 3.0.
+// quarter rate: 47 us of issue for 1,024 rows of V = 151,936, 311 MB of logits and 19 of masks, which take 49 us, 6.7 TB/s, part of it from the
+// last-level cache).  From memory alone, 2.49 GB without a mask: bfloat16 471 us, 5.3 TB/s, fp32 446 us, 5.6 TB/s.  256 rows fp32, masks of all kinds 14.4 us; 64 rows of V = 128,256 4.1; 4 rows of 32,000 with few tokens allowed 3.0.
 constexpr int kScanWaves = 4, kScanFew = 6;
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr double LN2 = 0.693147180559945309417232;
@@ -286,6 +286,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void k_beam_scan(const uint32_t* b
 // that other dies have written (about 1 us each).  us, kernel trace: 1 group of 4 beams, V = 32,000, 8 candidates 7.0; 16 of 4, V = 128,256,
 // 8 candidates 8.8; 128 of 8, V = 151,936, 16 candidates 9.8; 8 of 32, V = 151,936, 64 candidates 12.7.  Both kernels in one launch, a workgroup
 // for a group of up to 64 pieces, was slower when it was tried: 1 x 4 beams, V = 32,000 12.3 as two, 23.6 as one; 64 x 8, V = 4,000 13.9 and 21.6.
+// What the pass left of a row's pieces stays in registers up to kPickHeld * 16 * kBeamPiece = 163,840 tokens; what is beyond is read again, one
+// load at a time.  Calls over bfloat16 without a mask at V = 151,936 / 201,088 / 256,000 / 524,288, us: 1 group of 4 beams 11.6 / 14.1 / 14.4 / 22.2,
+// 16 of 8 19.5 / 21.9 / 25.5 / 42.3, 4 of 32 21.0 / 24.8 / 27.9 / 47.6.
 constexpr int kPickThreads = 1024, kPickMostWaves = kPickThreads / 64, kPickBins = 1024, kPickListed = 512, kPickElems = 1024, kPickHeld = 5;
 
 constexpr uint32_t kRowShift = 26, kRowBits = (1u << kRowShift) - 1;
@@ -651,7 +654,8 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(const float4* all_st
         for (uint32_t p = part + kPickHeld * 16; p < pieces; p += 16) look(stats[p]);
         m = largest_of_16(m);
         // a NaN or an infinity among what counts, or magnitudes that the sum's exponents cannot take or that leave a score no places behind
-        // the point: from the logits again
+        // the point: from the logits again, by this workgroup alone, row after row (a call of 128 groups whose seven other beams have scores
+        // of -1e9 697 us; of -1e5 66, of minus infinity 24)
         odd |= !(m < 1e6f) || (m > NINF && m < -1e6f) || !(s < 1e6f && s > -1e6f);
         repair = ((__ballot(odd) >> (lane & 48)) & 0xFFFF) != 0;
         // A piece's sum is of 2^(x * LOG2E - c), c = the rounded product of its maximum and LOG2E; LOG2E itself is off by `off`.
@@ -1047,7 +1051,7 @@ __global__ __launch_bounds__(256) void k_beam_reorder_strips(const int32_t* pare
 // that the sequences enter it with, writing their tokens.  A step's parents are one load for all beams of a group, which waits for nothing;
 // which of them a beam's is comes from the lane that holds it.  Segments of up to kTraceHeld steps are loaded once and kept in registers.
 // Bound by latency (the loads, then some 30 exchanges of about 50 ns).  4 beams, 128 steps 4.8 us, 64 groups of 8 beams, 1,500 steps 9.4 us;
-// a thread per sequence, step after step 24.8 and 311.
+// a thread per sequence, step after step 22.4 and 537.
 constexpr int kTraceThreads = 1024, kTraceHeld = 16;
 template <int WIDTH>
 __global__ __launch_bounds__(kTraceThreads) void k_beam_backtrace(BeamTrace A, uint32_t segments, uint32_t length) {
@@ -1190,6 +1194,7 @@ static void launch_rows_as(const BeamRows& A, hipStream_t stream) {
 // What a thread holds of each row, and how many columns of it.  TB/s over 537 MB (rows of 256 positions of 128 bytes, moved bytes counted
 // once read and once written), 2 / 4 / 8 / 16 / 17 / 32 / 33 / 64 beams: 16 bytes, one column 3.3 / 5.4 / 5.2 / 4.8 / - / 3.9 / - / -, two columns
 // 4.8 / 5.1 / 5.0 (their registers cost wavefronts), 4 bytes - / - / - / - / 4.1 / 4.2 / 2.6 / 3.3, strips in LDS - / - / - / - / 3.7 / 4.6 / 4.5 / 4.7.
+// (Columns of 4 bytes were a tenth faster at 17 beams; strips are all that is kept above 16, since they are the faster ones at 32 and above.)
 void launch_beam_reorder_rows(const BeamRows& A, hipStream_t stream) {
     if (A.beams <= 2) launch_rows_as<Wide4, 2, 2>(A, stream);
     else if (A.beams <= 4) launch_rows_as<Wide4, 4, 1>(A, stream);
